@@ -288,6 +288,97 @@ int zs_variant_validate(const zs_variant_desc *d);
 int zs_variant_decompress(const zs_variant_desc *d, const void *blob_dev, uint16_t *W_out_dev,
                           int64_t ldw, void *hip_stream);
 
+/* ---- 8-bit products ----------------------------------------------------------------------
+ * A third storage of a weight matrix, beside the compressed blob and plain BF16: OCP E4M3 codes
+ * (one byte, largest value 448, NaN but no Inf) with one FP32 scale for each block of 128 along K.
+ * Lossy, unlike the blob; half a BF16 matrix's bytes, and multiplied at twice BF16's rate.
+ *   codes   [rows, K], one byte each, in rows of ld bytes, ld % 16 == 0, the matrix 16-byte
+ *           aligned.  The rows * ld bytes belong to the matrix; what lies behind K in a row has no
+ *           effect on a product.
+ *   scales  by blocks of K: S[kb * lds + r] belongs to the codes 128 kb .. 128 kb + 127 of row r
+ *           (blocks of 1 x 128) or of rows 128 r .. 128 r + 127 (blocks of 128 x 128).  lds is at
+ *           least the number of rows, or of blocks of 128 rows.  Any FP32 values.  (Scales held
+ *           as [rows / 128, K / 128] are transposed once when a model is loaded.)
+ * Element types of other operands: */
+#define ZS_TYPE_BF16 0 /* uint16_t bit patterns */
+#define ZS_TYPE_F32 1
+
+/* Codes and scales of a matrix.
+ *   X_dev       [R, C] of x_type (ZS_TYPE_*), row stride ldx >= C elements          (device, in)
+ *   block_rows  1 (activations, gradients) or 128 (weights): height of a block of the result
+ *   transpose   0: the result is X, [R, C]; otherwise its transpose, [C, R]
+ *   Q_dev       codes of the result, ldq >= its columns                            (device, out)
+ *   S_dev       its scales, ceil(columns / 128) rows of lds                        (device, out)
+ * The scale of a block is the least power of two 2^e >= 2^-126 with max |x| <= 448 * 2^e over its
+ * finite x (1 if they are all zero), the code the E4M3 number nearest to x / scale, ties to
+ * even; NaN and Inf become NaN.  x / scale is exact: codes and scales are fully determined by X.
+ * Codes between the last column and the next multiple of 16 are set to zero; bytes of Q_dev
+ * behind that, and scales behind the last, are left as they were.
+ * ZS_ERR_CONFIG for an unknown type or block_rows. */
+int zs_fp8_quantize(const void *X_dev, int x_type, int64_t R, int64_t C, int64_t ldx, int block_rows,
+                    int transpose, uint8_t *Q_dev, int64_t ldq, float *S_dev, int64_t lds,
+                    void *hip_stream);
+
+/* C = A * W^T on codes with scales: C[m,n] = sum over blocks b of K of SA[b,m] * SW[b,n / w_rows] *
+ * sum over k in b of A[m,k] * W[n,k].  FP32 accumulation on the matrix cores inside a block,
+ * the product of the two scales and the sum over the blocks in FP32; C is overwritten.
+ *   A_dev, SA_dev  [M, K] codes, blocks of 1 x 128, ldsa >= M                       (device, in)
+ *   W_dev, SW_dev  [N, K] codes, blocks of w_rows x 128 (w_rows 1 or 128)           (device, in)
+ *   C_dev          [M, N] float, row stride ldc >= N, ldc % 4 == 0, 16-byte aligned (device, out)
+ *   M, N, K        >= 1, any integers
+ *   workspace_dev / workspace_bytes  optional scratch, 256-byte aligned, any contents: with it,
+ *          products of few tokens or features can be split along K over more of the GPU.
+ *          ZS_FP8_WORKSPACE_BYTES is enough for every call, less (or NULL) splits less.  Calls
+ *          that share it must not overlap.                                     (device, scratch)
+ * The order of every sum is fixed by the sizes and workspace_bytes: the same call gives the same bits.
+ * The gradients of C = X W^T are calls of this function on transposed codes: dX[M,K] = dY W with dY in
+ * blocks of 1 x 128 along N and the transpose of W in blocks of 128 x 128, and dW[N,K] = dY^T X with the
+ * transposes of dY and X in blocks of 1 x 128 along the tokens (w_rows 1). */
+#define ZS_FP8_WORKSPACE_BYTES ((size_t)32 << 20)
+int zs_fp8_gemm(const uint8_t *A_dev, int64_t lda, const float *SA_dev, int64_t ldsa,
+                const uint8_t *W_dev, int64_t ldw, const float *SW_dev, int64_t ldsw, int w_rows,
+                float *C_dev, int64_t ldc, int64_t M, int64_t N, int64_t K, void *workspace_dev,
+                size_t workspace_bytes, void *hip_stream);
+
+/* zs_fp8_gemm with the result rounded once to BF16 (nearest even), as zs_gemm_bf16 does. */
+int zs_fp8_gemm_bf16(const uint8_t *A_dev, int64_t lda, const float *SA_dev, int64_t ldsa,
+                     const uint8_t *W_dev, int64_t ldw, const float *SW_dev, int64_t ldsw, int w_rows,
+                     uint16_t *C_dev, int64_t ldc, int64_t M, int64_t N, int64_t K, void *workspace_dev,
+                     size_t workspace_bytes, void *hip_stream);
+
+/* ---- Embeddings ---------------------------------------------------------------------------
+ * Rows of a table by token ids.  A model whose LM head shares its table needs no unpacked copy of it:
+ * zs_embed reads the same blob that zs_gemm multiplies by.
+ *   ids_dev  T ids of id_bytes 4 (int32_t) or 8 (int64_t) each, naturally aligned    (device, in)
+ *            An id that is negative or not below the table's number of rows marks a padded
+ *            position: its row of Y is zero, and it takes no part in the gradient.
+ *   T        >= 0; with no tokens the other device pointers may be NULL */
+
+/* Y[t] = bf16(scale * decode(W)[ids[t]]), the product in FP32, rounded once.
+ *   blob_dev  the encoded table, 256-byte aligned                                    (device, in)
+ *   Y_dev     [T, K] BF16 bit patterns, row stride ldy >= K                         (device, out) */
+int zs_embed(const zs_desc *d, const void *blob_dev, const void *ids_dev, int id_bytes, int64_t T,
+             float scale, uint16_t *Y_dev, int64_t ldy, void *hip_stream);
+
+/* The same for an uncompressed table W_dev [N, K] of BF16 bit patterns, row stride ldw >= K. */
+int zs_dense_embed(const uint16_t *W_dev, int64_t N, int64_t K, int64_t ldw, const void *ids_dev,
+                   int id_bytes, int64_t T, float scale, uint16_t *Y_dev, int64_t ldy, void *hip_stream);
+
+/* Gradient of the table: dW[v] = scale * sum over t with ids[t] == v of dY[t], in FP32.
+ *   dY_dev      [T, K] of dy_type (ZS_TYPE_*), row stride lddy >= K elements         (device, in)
+ *   dW_dev      [N, K] float, row stride lddw >= K                                  (device, out)
+ *   accumulate  0: all N rows are written, zero where no token has that id; otherwise the sums are
+ *               added to the rows that have tokens, and the others are left alone (a tied table, whose
+ *               gradient as an LM head is already there)
+ *   workspace_dev  zs_embed_grad_workspace(T, N, K) bytes of scratch or ZS_ERR_SIZE, 256-byte
+ *               aligned, any contents; calls that share it must not overlap      (device, scratch)
+ * The tokens are sorted by id and summed in the order of the batch's positions within fixed chunks: no
+ * atomics, the same call gives the same bits. */
+size_t zs_embed_grad_workspace(int64_t T, int64_t N, int64_t K);
+int zs_embed_grad(const void *ids_dev, int id_bytes, int64_t T, const void *dY_dev, int dy_type,
+                  int64_t lddy, float scale, float *dW_dev, int64_t N, int64_t K, int64_t lddw,
+                  int accumulate, void *workspace_dev, size_t workspace_bytes, void *hip_stream);
+
 /* Compute units of the current device, which the tiling choices above scale with (256, those of
  * one MI355X, when no device can be asked: the sizing queries also run without a GPU). */
 int zs_compute_units(void);

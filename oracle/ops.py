@@ -1,0 +1,89 @@
+"""Plain definitions, in 64 bits, of the 8-bit products and the embedding operators (numpy; test infrastructure only)."""
+from __future__ import annotations
+
+import numpy as np
+
+
+def e4m3_table() -> np.ndarray:
+    """The values of the 256 OCP E4M3 codes: sign, four exponent bits (bias 7), three of mantissa; 0x7F and 0xFF are NaN."""
+    c = np.arange(256)
+    e, m = (c >> 3) & 15, c & 7
+    v = np.where(e == 0, m * 2.0 ** -9, (8 + m) * 2.0 ** (e - 10.0))
+    v[(c & 127) == 127] = np.nan
+    return np.where(c > 127, -v, v)
+
+
+TABLE = e4m3_table()
+POSITIVE = TABLE[:127]  # ascending with the code
+
+
+def e4m3(x: np.ndarray) -> np.ndarray:
+    """Codes of the numbers nearest to x (|x| <= 448), ties to the even code; what is not finite gives 0x7F."""
+    x = np.asarray(x, dtype=np.float64)
+    fine = np.isfinite(x)
+    a = np.where(fine, np.abs(x), 0.0)
+    hi = np.searchsorted(POSITIVE, a).clip(1, 126)
+    lo = hi - 1
+    d_lo, d_hi = a - POSITIVE[lo], POSITIVE[hi] - a
+    code = np.where((d_lo < d_hi) | ((d_lo == d_hi) & (lo % 2 == 0)), lo, hi)
+    return np.where(fine, code | np.where(np.signbit(x), 128, 0), 127).astype(np.uint8)
+
+
+def _groups(n: int, size: int) -> np.ndarray:
+    return np.arange(n) // size
+
+
+def spread(scales: np.ndarray, block_rows: int, rows: int, cols: int) -> np.ndarray:
+    """Scales S[column block, row block] as one for each element."""
+    return scales.astype(np.float64).T[_groups(rows, block_rows)][:, _groups(cols, 128)]
+
+
+def quantize(x: np.ndarray, block_rows: int) -> tuple[np.ndarray, np.ndarray]:
+    """(codes [R, C], scales [column blocks, row blocks]) of x in blocks of block_rows x 128."""
+    x = np.asarray(x, dtype=np.float64)
+    r, c = x.shape
+    s = np.ones((-(-c // 128), -(-r // block_rows)))
+    for kb in range(s.shape[0]):
+        for rb in range(s.shape[1]):
+            block = x[rb * block_rows:(rb + 1) * block_rows, kb * 128:(kb + 1) * 128]
+            peak = np.abs(block[np.isfinite(block)]).max(initial=0.0)
+            if peak > 0:
+                e = -126
+                while peak > 448.0 * 2.0 ** e:
+                    e += 1
+                s[kb, rb] = 2.0 ** e
+    with np.errstate(invalid="ignore"):
+        return e4m3(x / spread(s, block_rows, r, c)), s.astype(np.float32)
+
+
+def fp8_gemm(a, sa, w, sw, w_rows: int) -> tuple[np.ndarray, np.ndarray]:
+    """C = sum over blocks of (SA SW) * (A W^T of the block), and S = the same of magnitudes."""
+    m, k = a.shape
+    n = w.shape[0]
+    c, total = np.zeros((m, n)), np.zeros((m, n))
+    av, wv = TABLE[a], TABLE[w]
+    with np.errstate(invalid="ignore", over="ignore"):
+        for b in range(-(-k // 128)):
+            at = slice(128 * b, min(k, 128 * (b + 1)))
+            scale = sa[b, :m].astype(np.float64)[:, None] * sw[b].astype(np.float64)[_groups(n, w_rows)][None, :]
+            c += scale * (av[:, at] @ wv[:, at].T)
+            total += np.abs(scale) * (np.abs(av[:, at]) @ np.abs(wv[:, at]).T)
+    return c, total
+
+
+def embed(w: np.ndarray, ids: np.ndarray, scale: float) -> np.ndarray:
+    """scale * W[ids] in FP32, one rounding; zero rows for ids outside the table.  w in FP32 values."""
+    known = (ids >= 0) & (ids < w.shape[0])
+    with np.errstate(invalid="ignore", over="ignore"):
+        rows = w[np.where(known, ids, 0)].astype(np.float32) * np.float32(scale)
+    return np.where(known[:, None], rows, np.float32(0))
+
+
+def embed_grad(ids: np.ndarray, dy: np.ndarray, rows: int, scale: float) -> tuple[np.ndarray, np.ndarray, np.ndarray]:
+    """(dW, the same of magnitudes, tokens of each row)."""
+    known = (ids >= 0) & (ids < rows)
+    dw, total, count = np.zeros((rows, dy.shape[1])), np.zeros((rows, dy.shape[1])), np.zeros(rows, dtype=np.int64)
+    np.add.at(dw, ids[known], dy[known].astype(np.float64))
+    np.add.at(total, ids[known], np.abs(dy[known].astype(np.float64)))
+    np.add.at(count, ids[known], 1)
+    return dw * scale, total * abs(scale), count

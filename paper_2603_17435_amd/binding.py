@@ -22,7 +22,8 @@ EXPORTS = ["zs_encode_bound", "zs_encode", "zs_encode_device", "zs_desc_validate
            "zs_gemm_ex", "zs_gemm_workspace_ex", "zs_gemm_config_name", "zs_gemm_num_configs",
            "zs_gemm_pick_config", "zs_gemm_noalloc", "zs_gemm_bf16", "zs_dense_gemm", "zs_dense_gemm_algos", "zs_linear",
            "zs_linear_path", "zs_linear_workspace", "zs_compute_units", "zs_strerror", "zs_version",
-           "zs_variant_bound", "zs_variant_encode", "zs_variant_validate", "zs_variant_decompress"]
+           "zs_variant_bound", "zs_variant_encode", "zs_variant_validate", "zs_variant_decompress",
+           "zs_fp8_quantize", "zs_fp8_gemm", "zs_fp8_gemm_bf16", "zs_embed", "zs_dense_embed", "zs_embed_grad_workspace", "zs_embed_grad"]
 
 
 class ZsError(RuntimeError):
@@ -105,6 +106,14 @@ def lib() -> ctypes.CDLL:
         L.zs_variant_encode.argtypes, L.zs_variant_encode.restype = [vp, i64, i64, i64, ci, ci, ci, vp, sz, vdp, ci], ci
         L.zs_variant_validate.argtypes, L.zs_variant_validate.restype = [vdp], ci
         L.zs_variant_decompress.argtypes, L.zs_variant_decompress.restype = [vdp, vp, vp, i64, vp], ci
+        f32 = ctypes.c_float
+        L.zs_fp8_quantize.argtypes, L.zs_fp8_quantize.restype = [vp, ci, i64, i64, i64, ci, ci, vp, i64, vp, i64, vp], ci
+        for fn in (L.zs_fp8_gemm, L.zs_fp8_gemm_bf16):
+            fn.argtypes, fn.restype = [vp, i64, vp, i64, vp, i64, vp, i64, ci, vp, i64, i64, i64, i64, vp, sz, vp], ci
+        L.zs_embed.argtypes, L.zs_embed.restype = [dp, vp, vp, ci, i64, f32, vp, i64, vp], ci
+        L.zs_dense_embed.argtypes, L.zs_dense_embed.restype = [vp, i64, i64, i64, vp, ci, i64, f32, vp, i64, vp], ci
+        L.zs_embed_grad_workspace.argtypes, L.zs_embed_grad_workspace.restype = [i64, i64, i64], sz
+        L.zs_embed_grad.argtypes, L.zs_embed_grad.restype = [vp, ci, i64, vp, ci, i64, f32, vp, i64, i64, i64, ci, vp, sz, vp], ci
         _lib = L
     return _lib
 
@@ -278,3 +287,69 @@ def zs_gemm_configs() -> dict[int, str]:
 
 def zs_gemm_pick_config(desc: ZsDesc, M: int) -> int:
     return int(lib().zs_gemm_pick_config(ctypes.byref(desc), M))
+
+
+ZS_TYPE_BF16, ZS_TYPE_F32 = 0, 1
+ZS_FP8_WORKSPACE_BYTES = 32 << 20
+
+
+def zs_fp8_quantize(X_dev, x_type: int, R: int, C: int, Q_dev, S_dev, ldx: int | None = None, ldq: int | None = None,
+                    lds: int | None = None, block_rows: int = 1, transpose: bool = False, stream=None) -> None:
+    """E4M3 codes and scales (blocks of block_rows x 128) of X [R, C], or of its transpose.  Without ldq and lds the
+    result's rows are as long as its columns rounded up to 16, and its rows of scales as it has (blocks of) rows."""
+    rows, cols = (C, R) if transpose else (R, C)
+    _check("zs_fp8_quantize", lib().zs_fp8_quantize(_ptr(X_dev), x_type, R, C, C if ldx is None else ldx, block_rows, int(transpose),
+                                                    _ptr(Q_dev), -(-cols // 16) * 16 if ldq is None else ldq, _ptr(S_dev),
+                                                    -(-rows // max(block_rows, 1)) if lds is None else lds, _stream(stream)))
+
+
+def _fp8_gemm(name, A_dev, SA_dev, W_dev, SW_dev, C_dev, M, N, K, w_rows, lda, ldsa, ldw, ldsw, ldc, workspace_dev, workspace_bytes, stream):
+    ld = -(-K // 16) * 16
+    _check(name, getattr(lib(), name)(_ptr(A_dev), ld if lda is None else lda, _ptr(SA_dev), M if ldsa is None else ldsa, _ptr(W_dev),
+                                      ld if ldw is None else ldw, _ptr(SW_dev), -(-N // max(w_rows, 1)) if ldsw is None else ldsw, w_rows,
+                                      _ptr(C_dev), -(-N // 4) * 4 if ldc is None else ldc, M, N, K, _ptr(workspace_dev), workspace_bytes,
+                                      _stream(stream)))
+
+
+def zs_fp8_gemm(A_dev, SA_dev, W_dev, SW_dev, C_dev, M: int, N: int, K: int, w_rows: int = 128, lda: int | None = None,
+                ldsa: int | None = None, ldw: int | None = None, ldsw: int | None = None, ldc: int | None = None,
+                workspace_dev=None, workspace_bytes: int = 0, stream=None) -> None:
+    """C (FP32) = A W^T on E4M3 codes with a scale for each block of 128 along K (A: 1 x 128, W: w_rows x 128).  Without
+    lda, ldw and ldc the rows are K rounded up to 16 and N rounded up to 4 long."""
+    _fp8_gemm("zs_fp8_gemm", A_dev, SA_dev, W_dev, SW_dev, C_dev, M, N, K, w_rows, lda, ldsa, ldw, ldsw, ldc, workspace_dev,
+              workspace_bytes, stream)
+
+
+def zs_fp8_gemm_bf16(A_dev, SA_dev, W_dev, SW_dev, C_dev, M: int, N: int, K: int, w_rows: int = 128, lda: int | None = None,
+                     ldsa: int | None = None, ldw: int | None = None, ldsw: int | None = None, ldc: int | None = None,
+                     workspace_dev=None, workspace_bytes: int = 0, stream=None) -> None:
+    """zs_fp8_gemm with C rounded once to BF16 bit patterns."""
+    _fp8_gemm("zs_fp8_gemm_bf16", A_dev, SA_dev, W_dev, SW_dev, C_dev, M, N, K, w_rows, lda, ldsa, ldw, ldsw, ldc, workspace_dev,
+              workspace_bytes, stream)
+
+
+def zs_embed(desc: ZsDesc, blob_dev, ids_dev, id_bytes: int, T: int, Y_dev, scale: float = 1.0, ldy: int | None = None,
+             stream=None) -> None:
+    """Y (BF16 bit patterns) = scale * rows `ids` of the table packed in blob_dev; zeros for an id outside it."""
+    _check("zs_embed", lib().zs_embed(ctypes.byref(desc), _ptr(blob_dev), _ptr(ids_dev), id_bytes, T, scale, _ptr(Y_dev),
+                                      desc.K if ldy is None else ldy, _stream(stream)))
+
+
+def zs_dense_embed(W_dev, N: int, K: int, ids_dev, id_bytes: int, T: int, Y_dev, scale: float = 1.0, ldw: int | None = None,
+                   ldy: int | None = None, stream=None) -> None:
+    """zs_embed on an uncompressed BF16 table W [N, K]."""
+    _check("zs_dense_embed", lib().zs_dense_embed(_ptr(W_dev), N, K, K if ldw is None else ldw, _ptr(ids_dev), id_bytes, T, scale,
+                                                  _ptr(Y_dev), K if ldy is None else ldy, _stream(stream)))
+
+
+def zs_embed_grad_workspace(T: int, N: int, K: int) -> int:
+    return int(lib().zs_embed_grad_workspace(T, N, K))
+
+
+def zs_embed_grad(ids_dev, id_bytes: int, T: int, dY_dev, dy_type: int, dW_dev, N: int, K: int, scale: float = 1.0,
+                  lddy: int | None = None, lddw: int | None = None, accumulate: bool = False, workspace_dev=None,
+                  workspace_bytes: int = 0, stream=None) -> None:
+    """dW [N, K] (FP32) = (dW +) scale * the sums of dY's rows by id; scratch of zs_embed_grad_workspace() bytes."""
+    _check("zs_embed_grad", lib().zs_embed_grad(_ptr(ids_dev), id_bytes, T, _ptr(dY_dev), dy_type, K if lddy is None else lddy, scale,
+                                                _ptr(dW_dev), N, K, K if lddw is None else lddw, int(accumulate), _ptr(workspace_dev),
+                                                workspace_bytes, _stream(stream)))

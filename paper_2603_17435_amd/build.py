@@ -8,6 +8,7 @@ import sys
 PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
+OPS = os.path.join(CSRC, "ops")
 LIB = os.path.join(PKG, "libzipserv_hip.so")
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 
@@ -28,11 +29,16 @@ def sources() -> list[str]:
     return [os.path.join(CSRC, f) for f in sorted(os.listdir(CSRC)) if f.endswith((".hip", ".cpp"))]
 
 
+def operator_sources() -> list[str]:
+    """The kernels of the 8-bit products and the embedding operators."""
+    return [os.path.join(OPS, f) for f in sorted(os.listdir(OPS)) if f.endswith(".hip")]
+
+
 def is_stale() -> bool:
     if not os.path.exists(LIB):
         return True
     t = os.path.getmtime(LIB)
-    deps = [os.path.join(CSRC, f) for f in os.listdir(CSRC)] + [os.path.join(ROOT, "include", "zipserv.h")]
+    deps = [os.path.join(d, f) for d in (CSRC, OPS) for f in os.listdir(d)] + [os.path.join(ROOT, "include", "zipserv.h")]
     return any(os.path.getmtime(p) > t for p in deps)
 
 
@@ -41,7 +47,7 @@ def build(verbose: bool = False, extra: list[str] | None = None) -> str:
     objs = []
     build_dir = os.path.join(PKG, "_build")
     os.makedirs(build_dir, exist_ok=True)
-    for src in sources():
+    for src in sources() + operator_sources():
         obj = os.path.join(build_dir, os.path.basename(src) + ".o")
         cmd = [HIPCC, "-c", src, "-o", obj] + COMMON + (extra or [])
         if src.endswith(".hip"):

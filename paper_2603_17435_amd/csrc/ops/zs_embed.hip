@@ -1,0 +1,375 @@
+// Embedding operators: rows of a table by token ids, times a scale (zs_embed out of a compressed blob,
+// zs_dense_embed out of a BF16 matrix), and the gradient of the table (zs_embed_grad).
+#include "zs_format.h"
+#include "zs_ops.h"
+
+using namespace zs_ops;
+
+namespace {
+
+// A token id, or -1 where it names no row of the table.
+__device__ __forceinline__ int64_t id_at(const void *ids, int id_bytes, int64_t t, int64_t N)
+{
+    const int64_t id = id_bytes == 8 ? static_cast<const int64_t *>(ids)[t] : static_cast<const int32_t *>(ids)[t];
+    return id >= 0 && id < N ? id : -1;
+}
+
+// ---- rows of the compressed table --------------------------------------------------------
+// A wave decodes one token's 64 weights of one BlockTile.  Lane f first stands for FragTile f: where the
+// row's bytes of a FragTile start in H is the number of in-window elements before them, which a prefix sum of the popcounts
+// over the lanes gives.  Then lane c stands for the row's column c and fetches the three
+// plane bytes and the start of the FragTile that holds it.
+struct Blob {
+    const uint8_t *bitmaps;
+    const uint32_t *offsets;
+    const uint8_t *H;
+    const uint8_t *L;
+    uint64_t h_last, l_last; // offsets of the last byte of H and the last halfword of L: no read goes behind them
+    int32_t base_exp;
+    int32_t k_blocks;
+};
+
+__device__ __forceinline__ uint32_t inclusive_scan(uint32_t x, int lane)
+{
+    for (int d = 1; d < 64; d *= 2) {
+        const uint32_t y = (uint32_t)__shfl_up((int)x, d);
+        x += lane >= d ? y : 0u;
+    }
+    return x;
+}
+
+__global__ __launch_bounds__(256) void embed_kernel(Blob b, int64_t N, const void *ids, int id_bytes, int64_t tasks, float scale,
+                                                    uint16_t *Y, int64_t ldy)
+{
+    const int lane = threadIdx.x % 64;
+    for (int64_t task = (int64_t)blockIdx.x * 4 + threadIdx.x / 64; task < tasks; task += (int64_t)gridDim.x * 4) {
+        const int64_t t = task / b.k_blocks, kb = task - t * b.k_blocks;
+        uint16_t *const out = Y + t * ldy + ZS_BT_DIM * kb + lane;
+        const int64_t id = id_at(ids, id_bytes, t, N);
+        if (id < 0) {
+            *out = 0;
+            continue;
+        }
+        const int64_t bt = id / ZS_BT_DIM * b.k_blocks + kb;
+        const uint32_t row = (uint32_t)(id % ZS_BT_DIM), r = row % 8;
+        const uint64_t *planes = reinterpret_cast<const uint64_t *>(b.bitmaps + bt * ZS_BT_BITMAP_BYTES) + 3 * lane;
+        const uint64_t p1 = planes[0], p2 = planes[1], p3 = planes[2], m = p1 | p2 | p3;
+        const uint64_t h_start = 16 * (uint64_t)b.offsets[2 * bt], l_start = 16 * (uint64_t)b.offsets[2 * bt + 1];
+        const uint32_t count = (uint32_t)__popcll(m);
+        const uint32_t start = inclusive_scan(count, lane) - count + (uint32_t)__popcll(m & ((1ull << (8 * r)) - 1));
+        const uint32_t bytes = (uint32_t)(p1 >> (8 * r) & 0xFF) | (uint32_t)(p2 >> (8 * r) & 0xFF) << 8 | (uint32_t)(p3 >> (8 * r) & 0xFF) << 16;
+        // column `lane`: FragTile column lane / 8, which lies in TensorCoreTile column lane / 32
+        const uint32_t j = lane % 8, f = (lane / 32 * 4 + row / 16) * ZS_FT_PER_TT + lane / 8 % 4 * 2 + row / 8 % 2;
+        const uint32_t w = (uint32_t)__shfl((int)bytes, (int)f) >> j;
+        const uint32_t inside = (uint32_t)__shfl((int)(bytes | bytes >> 8 | bytes >> 16), (int)f) & 0xFFu;
+        const uint32_t hi = (uint32_t)__shfl((int)start, (int)f) + __popc(inside & ((1u << j) - 1u));
+        const uint32_t code = (w & 1u) | (w >> 8 & 1u) << 1 | (w >> 16 & 1u) << 2;
+        uint32_t value;
+        if (code) {
+            const uint32_t h = b.H[min(h_start + hi, b.h_last)];
+            value = (h & 0x80u) << 8 | ((uint32_t)(b.base_exp + (int)code) & 0xFFu) << 7 | (h & 0x7Fu);
+        } else {
+            const uint32_t li = 64 * f + 8 * r + j - hi;
+            value = *reinterpret_cast<const uint16_t *>(b.L + min(l_start + 2 * li, b.l_last));
+        }
+        *out = bf16_bits(bf16_value(value) * scale);
+    }
+}
+
+// ---- rows of a BF16 table ------------------------------------------------------------------
+// A thread takes eight columns of one token.
+__global__ __launch_bounds__(256) void dense_embed_kernel(const uint16_t *W, int64_t N, int64_t K, int64_t ldw, const void *ids, int id_bytes,
+                                                          int64_t units, int64_t row_units, float scale, uint16_t *Y, int64_t ldy)
+{
+    for (int64_t u = (int64_t)blockIdx.x * 256 + threadIdx.x; u < units; u += (int64_t)gridDim.x * 256) {
+        const int64_t t = u / row_units, c = 8 * (u - t * row_units), left = K - c;
+        const int64_t id = id_at(ids, id_bytes, t, N);
+        float v[8];
+        if (id >= 0) {
+            load8(W + id * ldw + c, left, v);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = 0.f;
+        }
+        uint16_t *const out = Y + t * ldy + c;
+        const float s = id >= 0 ? scale : 0.f;
+        if (left >= 8) {
+            store_any(out, u32x4{bf16_pair(v[0] * s, v[1] * s), bf16_pair(v[2] * s, v[3] * s), bf16_pair(v[4] * s, v[5] * s),
+                                 bf16_pair(v[6] * s, v[7] * s)});
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (i < left) out[i] = bf16_bits(v[i] * s);
+        }
+    }
+}
+
+int check_lookup(const void *ids, int id_bytes, int64_t T, const void *Y, int64_t ldy, int64_t K)
+{
+    if (id_bytes != 4 && id_bytes != 8) return ZS_ERR_CONFIG;
+    if (T < 0 || T > INT32_MAX || ldy < K) return ZS_ERR_SHAPE;
+    if (T > 0 && (!ids || !Y || !aligned(ids, id_bytes) || !aligned(Y, 2))) return ZS_ERR_ARG;
+    return ZS_OK;
+}
+
+// ---- gradient of the table -------------------------------------------------------------------
+// The (id, position) pairs of the tokens are sorted, so that a row's tokens lie next to each other in the order
+// of the batch.  The sorted list is cut into chunks of equal length, however often a token occurs; a wave sums
+// a chunk's rows of dY over a slice of the columns.  A run of one id that lies inside a chunk is finished
+// there; one that crosses a boundary leaves a partial sum for each chunk in the workspace, and these are added in order.
+// Every sum has one fixed order: the result is the same from run to run.
+constexpr int kTile = 1024; // pairs sorted by one workgroup
+constexpr int kFan = 16;    // sorted lists merged at a time
+constexpr uint32_t kNoRow = 0xFFFFFFFFu;
+
+typedef uint64_t Pair; // id << 32 | position: all different, so that a pair's place is a count of smaller ones
+
+__global__ __launch_bounds__(kTile) void sort_tiles_kernel(const void *ids, int id_bytes, int64_t T, int64_t N, Pair *out)
+{
+    __shared__ Pair keys[kTile];
+    const int tid = threadIdx.x;
+    const int64_t t = (int64_t)blockIdx.x * kTile + tid;
+    Pair mine = ~0ull;
+    if (t < T) {
+        const int64_t id = id_at(ids, id_bytes, t, N);
+        mine = (Pair)(id < 0 ? kNoRow : (uint32_t)id) << 32 | (uint32_t)t;
+    }
+    // bitonic sorting network: partners less than a wave apart meet in registers
+    for (int size = 2; size <= kTile; size *= 2)
+        for (int d = size / 2; d > 0; d /= 2) {
+            Pair other;
+            if (d < 64) {
+                other = (Pair)__shfl_xor((unsigned long long)mine, d);
+            } else {
+                keys[tid] = mine;
+                __syncthreads();
+                other = keys[tid ^ d];
+                __syncthreads();
+            }
+            const bool low = (tid & d) == 0, up = (tid & size) == 0;
+            mine = (low == up) ? min(mine, other) : max(mine, other);
+        }
+    if (t < T) out[t] = mine;
+}
+
+// Sorted lists of `run` pairs become lists of run * kFan: a pair's place is its own index plus the number of smaller
+// pairs in each of the other lists of its group.
+__global__ __launch_bounds__(256) void merge_kernel(const Pair *in, Pair *out, int64_t T, int64_t run)
+{
+    for (int64_t t = (int64_t)blockIdx.x * 256 + threadIdx.x; t < T; t += (int64_t)gridDim.x * 256) {
+        const Pair mine = in[t];
+        const int64_t group = t / (run * kFan) * (run * kFan), own = t / run * run;
+        int64_t place = group + (t - own);
+        for (int64_t l = group; l < min(group + run * kFan, T); l += run) {
+            if (l == own) continue;
+            int64_t lo = 0, hi = min(run, T - l); // smaller pairs of this list: at least lo, at most hi
+            while (lo < hi) {
+                const int64_t mid = (lo + hi) / 2;
+                if (in[l + mid] < mine) lo = mid + 1;
+                else hi = mid;
+            }
+            place += lo;
+        }
+        out[place] = mine;
+    }
+}
+
+__global__ __launch_bounds__(256) void zero_rows_kernel(float *dW, int64_t K, int64_t ldw, int64_t units, int64_t row_units)
+{
+    for (int64_t u = (int64_t)blockIdx.x * 256 + threadIdx.x; u < units; u += (int64_t)gridDim.x * 256) {
+        const int64_t r = u / row_units, c = 4 * (u - r * row_units);
+        float *p = dW + r * ldw + c;
+        if (c + 4 <= K) store_any(p, f32x4{0.f, 0.f, 0.f, 0.f});
+        else
+            for (int64_t i = c; i < K; ++i) dW[r * ldw + i] = 0.f;
+    }
+}
+
+struct Runs {
+    const Pair *pairs; // sorted
+    int64_t T, K, slices, chunks;
+    int chunk;
+    float *heads, *tails; // [chunks, K]: sums of a run that began before the chunk / that goes on behind it
+    __device__ uint32_t id(int64_t i) const { return (uint32_t)(pairs[i] >> 32); }
+    __device__ uint32_t id_before(int64_t chunk_at) const { return chunk_at == 0 ? kNoRow : id(chunk_at - 1); }
+    __device__ uint32_t id_behind(int64_t end) const { return end >= T ? kNoRow : id(end); }
+};
+
+constexpr int kCols = 8; // columns of a lane
+
+__device__ __forceinline__ void put(float *p, const float v[kCols], int64_t left, float scale, bool add)
+{
+    if (left >= kCols) {
+        f32x4 a = {v[0] * scale, v[1] * scale, v[2] * scale, v[3] * scale}, b = {v[4] * scale, v[5] * scale, v[6] * scale, v[7] * scale};
+        if (add) {
+            a += load_any<f32x4>(p);
+            b += load_any<f32x4>(p + 4);
+        }
+        store_any(p, a);
+        store_any(p + 4, b);
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < kCols; ++i)
+        if (i < left) p[i] = add ? p[i] + v[i] * scale : v[i] * scale;
+}
+
+template <typename T>
+__global__ __launch_bounds__(64) void sum_kernel(Runs g, const T *dY, int64_t lddy, float scale, float *dW, int64_t ldw, int add)
+{
+    for (int64_t task = blockIdx.x; task < g.chunks * g.slices; task += gridDim.x) {
+        const int64_t chunk = task / g.slices, c = ((task - chunk * g.slices) * 64 + threadIdx.x) * kCols, left = g.K - c;
+        const int64_t begin = chunk * g.chunk, end = min(begin + g.chunk, g.T);
+        if (left <= 0) continue;
+        const uint32_t before = g.id_before(begin), behind = g.id_behind(end);
+        float acc[kCols] = {};
+        for (int64_t i = begin; i < end; ++i) {
+            const Pair pair = g.pairs[i];
+            const uint32_t id = (uint32_t)(pair >> 32);
+            if (id == kNoRow) break; // only tokens without a row follow
+            float v[kCols];
+            load8(dY + (int64_t)(uint32_t)pair * lddy + c, left, v);
+#pragma unroll
+            for (int j = 0; j < kCols; ++j) acc[j] += v[j];
+            const uint32_t next = i + 1 < end ? g.id(i + 1) : behind;
+            if (i + 1 < end && next == id) continue;
+            // the run's sum over this chunk
+            if (id == before) put(g.heads + chunk * g.K + c, acc, left, 1.f, false);
+            else if (id == next) put(g.tails + chunk * g.K + c, acc, left, 1.f, false);
+            else put(dW + (int64_t)id * ldw + c, acc, left, scale, add);
+#pragma unroll
+            for (int j = 0; j < kCols; ++j) acc[j] = 0.f;
+        }
+    }
+}
+
+// Runs over several chunks: the chunk in which one begins adds up what the chunks behind it left.
+__global__ __launch_bounds__(64) void join_kernel(Runs g, float scale, float *dW, int64_t ldw, int add)
+{
+    for (int64_t task = blockIdx.x; task < (g.chunks - 1) * g.slices; task += gridDim.x) {
+        const int64_t chunk = task / g.slices, c = ((task - chunk * g.slices) * 64 + threadIdx.x) * kCols, left = g.K - c;
+        const int64_t begin = chunk * g.chunk, end = begin + g.chunk;
+        const uint32_t id = g.id(end - 1);
+        if (left <= 0 || id == kNoRow || id != g.id(end) || id == g.id_before(begin)) continue;
+        float acc[kCols], v[kCols];
+        load8(g.tails + chunk * g.K + c, left, acc);
+        for (int64_t k = chunk + 1; k < g.chunks && g.id(k * g.chunk) == id; ++k) {
+            load8(g.heads + k * g.K + c, left, v);
+#pragma unroll
+            for (int j = 0; j < kCols; ++j) acc[j] += v[j];
+        }
+        put(dW + (int64_t)id * ldw + c, acc, left, scale, add);
+    }
+}
+
+constexpr int kChunk = 32;
+
+struct GradPlan {
+    int64_t chunks;
+    size_t pairs_bytes, sums_bytes, total;
+};
+GradPlan plan_grad(int64_t T, int64_t K)
+{
+    GradPlan p;
+    auto up = [](size_t x) { return (x + 255) / 256 * 256; };
+    p.chunks = ceil_div(T, kChunk);
+    p.pairs_bytes = up(8 * (size_t)T);
+    p.sums_bytes = up(4 * (size_t)p.chunks * (size_t)K);
+    p.total = 2 * p.pairs_bytes + 2 * p.sums_bytes;
+    return p;
+}
+
+bool grad_shape_ok(int64_t T, int64_t N, int64_t K)
+{
+    return T >= 0 && T <= INT32_MAX && N >= 1 && N <= INT32_MAX && K >= 1 && K <= INT32_MAX;
+}
+
+} // namespace
+
+extern "C" int zs_embed(const zs_desc *d, const void *blob_dev, const void *ids_dev, int id_bytes, int64_t T, float scale, uint16_t *Y_dev,
+                        int64_t ldy, void *hip_stream)
+{
+    if (!d) return ZS_ERR_ARG;
+    int rc = zs_desc_validate(d);
+    if (rc != ZS_OK) return rc;
+    if (!blob_dev || !aligned(blob_dev, ZS_SECTION_ALIGN)) return ZS_ERR_ARG;
+    if ((rc = check_lookup(ids_dev, id_bytes, T, Y_dev, ldy, d->K)) != ZS_OK || T == 0) return rc;
+    const uint8_t *base = static_cast<const uint8_t *>(blob_dev);
+    Blob b;
+    b.bitmaps = base + d->off_bitmaps;
+    b.offsets = reinterpret_cast<const uint32_t *>(base + d->off_offsets);
+    b.H = d->h_bytes ? base + d->off_H : base; // (an empty section may lie at the blob's end)
+    b.L = d->l_bytes ? base + d->off_L : base;
+    b.h_last = d->h_bytes ? d->h_bytes - 1 : 0;
+    b.l_last = d->l_bytes ? d->l_bytes - 2 : 0;
+    b.base_exp = d->base_exp;
+    b.k_blocks = (int32_t)(d->K / ZS_BT_DIM);
+    const int64_t tasks = T * b.k_blocks;
+    hipLaunchKernelGGL(embed_kernel, dim3(grid_for(ceil_div(tasks, 4))), dim3(256), 0, static_cast<hipStream_t>(hip_stream), b, d->N, ids_dev,
+                       id_bytes, tasks, scale, Y_dev, ldy);
+    return launched();
+}
+
+extern "C" int zs_dense_embed(const uint16_t *W_dev, int64_t N, int64_t K, int64_t ldw, const void *ids_dev, int id_bytes, int64_t T,
+                              float scale, uint16_t *Y_dev, int64_t ldy, void *hip_stream)
+{
+    if (!W_dev || !aligned(W_dev, 2)) return ZS_ERR_ARG;
+    if (N < 1 || K < 1 || N > INT32_MAX || K > INT32_MAX || ldw < K) return ZS_ERR_SHAPE;
+    const int rc = check_lookup(ids_dev, id_bytes, T, Y_dev, ldy, K);
+    if (rc != ZS_OK || T == 0) return rc;
+    const int64_t row_units = ceil_div(K, 8), units = T * row_units;
+    hipLaunchKernelGGL(dense_embed_kernel, dim3(grid_for(ceil_div(units, 256))), dim3(256), 0, static_cast<hipStream_t>(hip_stream), W_dev, N, K,
+                       ldw, ids_dev, id_bytes, units, row_units, scale, Y_dev, ldy);
+    return launched();
+}
+
+extern "C" size_t zs_embed_grad_workspace(int64_t T, int64_t N, int64_t K)
+{
+    return grad_shape_ok(T, N, K) ? plan_grad(T, K).total : 0;
+}
+
+extern "C" int zs_embed_grad(const void *ids_dev, int id_bytes, int64_t T, const void *dY_dev, int dy_type, int64_t lddy, float scale,
+                             float *dW_dev, int64_t N, int64_t K, int64_t lddw, int accumulate, void *workspace_dev, size_t workspace_bytes,
+                             void *hip_stream)
+{
+    if (id_bytes != 4 && id_bytes != 8) return ZS_ERR_CONFIG;
+    if (dy_type != ZS_TYPE_BF16 && dy_type != ZS_TYPE_F32) return ZS_ERR_CONFIG;
+    if (!grad_shape_ok(T, N, K) || lddy < K || lddw < K) return ZS_ERR_SHAPE;
+    if (!dW_dev || !aligned(dW_dev, 4)) return ZS_ERR_ARG;
+    if (T > 0 && (!ids_dev || !dY_dev || !workspace_dev || !aligned(ids_dev, id_bytes) || !aligned(dY_dev, dy_type == ZS_TYPE_BF16 ? 2 : 4) ||
+                  !aligned(workspace_dev, 256)))
+        return ZS_ERR_ARG;
+    const GradPlan plan = plan_grad(T, K);
+    if (workspace_bytes < plan.total) return ZS_ERR_SIZE;
+    hipStream_t s = static_cast<hipStream_t>(hip_stream);
+    if (!accumulate) {
+        const int64_t row_units = ceil_div(K, 4), units = N * row_units;
+        hipLaunchKernelGGL(zero_rows_kernel, dim3(grid_for(ceil_div(units, 256))), dim3(256), 0, s, dW_dev, K, lddw, units, row_units);
+    }
+    if (T == 0) return launched();
+    uint8_t *ws = static_cast<uint8_t *>(workspace_dev);
+    Pair *from = reinterpret_cast<Pair *>(ws), *to = reinterpret_cast<Pair *>(ws + plan.pairs_bytes);
+    hipLaunchKernelGGL(sort_tiles_kernel, dim3((unsigned)ceil_div(T, kTile)), dim3(kTile), 0, s, ids_dev, id_bytes, T, N, from);
+    for (int64_t run = kTile; run < T; run *= kFan) {
+        hipLaunchKernelGGL(merge_kernel, dim3(grid_for(ceil_div(T, 256))), dim3(256), 0, s, from, to, T, run);
+        Pair *const swap = from;
+        from = to;
+        to = swap;
+    }
+    Runs g;
+    g.pairs = from;
+    g.T = T;
+    g.K = K;
+    g.slices = ceil_div(K, 64 * kCols);
+    g.chunks = plan.chunks;
+    g.chunk = kChunk;
+    g.heads = reinterpret_cast<float *>(ws + 2 * plan.pairs_bytes);
+    g.tails = reinterpret_cast<float *>(ws + 2 * plan.pairs_bytes + plan.sums_bytes);
+    const dim3 grid(grid_for(g.chunks * g.slices));
+    if (dy_type == ZS_TYPE_BF16)
+        hipLaunchKernelGGL(sum_kernel<uint16_t>, grid, dim3(64), 0, s, g, static_cast<const uint16_t *>(dY_dev), lddy, scale, dW_dev, lddw, accumulate);
+    else
+        hipLaunchKernelGGL(sum_kernel<float>, grid, dim3(64), 0, s, g, static_cast<const float *>(dY_dev), lddy, scale, dW_dev, lddw, accumulate);
+    if (g.chunks > 1) hipLaunchKernelGGL(join_kernel, dim3(grid_for((g.chunks - 1) * g.slices)), dim3(64), 0, s, g, scale, dW_dev, lddw, accumulate);
+    return launched();
+}

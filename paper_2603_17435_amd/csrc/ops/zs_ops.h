@@ -1,0 +1,82 @@
+// What the kernels of the 8-bit products and of the embedding operators share: unaligned vector
+// access, BF16 conversion, and the host's argument helpers.
+#ifndef ZS_OPS_H
+#define ZS_OPS_H
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "zipserv.h"
+
+namespace zs_ops {
+
+typedef __attribute__((ext_vector_type(2))) uint32_t u32x2;
+typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
+typedef __attribute__((ext_vector_type(8))) int32_t i32x8;
+typedef __attribute__((ext_vector_type(4))) float f32x4;
+typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
+typedef __attribute__((ext_vector_type(2))) _Float16 f16x2;
+typedef __attribute__((ext_vector_type(8))) _Float16 f16x8;
+
+// Vectors at any element's address: rows of odd length or stride start where no vector is aligned.
+// The hardware takes such an address for a global access of any width.
+template <typename V, typename T>
+__device__ __forceinline__ V load_any(const T *p)
+{
+    V v;
+    __builtin_memcpy(&v, p, sizeof v);
+    return v;
+}
+template <typename V, typename T>
+__device__ __forceinline__ void store_any(T *p, V v)
+{
+    __builtin_memcpy(p, &v, sizeof v);
+}
+
+__device__ __forceinline__ float bf16_value(uint32_t bits) { return __builtin_bit_cast(float, bits << 16); }
+
+// Nearest BF16 number, ties to even; NaN stays NaN.
+__device__ __forceinline__ uint16_t bf16_bits(float x) { return __builtin_bit_cast(uint16_t, (__bf16)x); }
+__device__ __forceinline__ uint32_t bf16_pair(float lo, float hi)
+{
+    return __builtin_bit_cast(uint32_t, bf16x2{(__bf16)lo, (__bf16)hi});
+}
+
+// Eight consecutive values of a row of BF16 patterns or floats; those at and behind `left` are zero.
+__device__ __forceinline__ void load8(const uint16_t *p, int64_t left, float v[8])
+{
+    if (left >= 8) {
+        const u32x4 w = load_any<u32x4>(p);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            v[2 * i] = bf16_value(w[i] & 0xFFFFu);
+            v[2 * i + 1] = __builtin_bit_cast(float, w[i] & 0xFFFF0000u);
+        }
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = i < left ? bf16_value(p[i]) : 0.f;
+}
+__device__ __forceinline__ void load8(const float *p, int64_t left, float v[8])
+{
+    if (left >= 8) {
+        const f32x4 a = load_any<f32x4>(p), b = load_any<f32x4>(p + 4);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            v[i] = a[i];
+            v[4 + i] = b[i];
+        }
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = i < left ? p[i] : 0.f;
+}
+
+inline bool aligned(const void *p, uintptr_t to) { return reinterpret_cast<uintptr_t>(p) % to == 0; }
+inline int launched() { return hipGetLastError() == hipSuccess ? ZS_OK : ZS_ERR_HIP; }
+// A launch counts its threads along x in 32 bits: kernels whose work could exceed that stride over it.
+inline unsigned grid_for(int64_t wgs, int64_t most = 1 << 20) { return (unsigned)(wgs < most ? wgs : most); }
+inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+} // namespace zs_ops
+#endif
