@@ -3,11 +3,16 @@
 // FP32 accumulator.
 #include "zs_ops.h"
 
+#include <algorithm>
+#include <type_traits>
+
 using namespace zs_ops;
 
 namespace {
 
 constexpr int kBlock = 128;
+constexpr int64_t kMaxLd = (int64_t)1 << 23;
+constexpr int64_t kMaxTiles = (int64_t)1 << 22; // of one launch: its threads are counted in 32 bits
 
 struct Product {
     const uint8_t *A, *W;
@@ -91,19 +96,249 @@ __global__ __launch_bounds__(256) void product_kernel(Product p, OUT *C, int64_t
     }
 }
 
+// ---- tiles through LDS ---------------------------------------------------------------------
+// A workgroup of WM x WN waves computes (16 TM WM) tokens x (16 TN WN) features over the blocks [kb0, kb1) of K.  Each
+// block's codes and scales go from memory straight to LDS (two buffers: block b + 1 is under way while b is
+// multiplied, one barrier a block).  A row's eight chunks of 16 bytes lie in the order chunk ^ (row % 8), so that
+// the sixteen rows of an operand are read without bank conflicts.
+constexpr int kRowBytes = 128;
+
+// 64 lanes x 16 (or 4) bytes from base + at to the 1 KB (256 bytes) of LDS at `to`.  Not tracked by the compiler: arrived().
+__device__ __forceinline__ void fetch16(const void *base, uint32_t at, uint32_t to)
+{
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(at), "s"(base), "s"(to) : "memory", "m0");
+}
+__device__ __forceinline__ void fetch4(const void *base, uint32_t at, uint32_t to)
+{
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dword %0, %1" ::"v"(at), "s"(base), "s"(to) : "memory", "m0");
+}
+__device__ __forceinline__ void arrived() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+__device__ __forceinline__ void barrier()
+{
+    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+}
+
+typedef const __attribute__((address_space(3))) u32x4 *LdsU32x4;
+typedef const __attribute__((address_space(3))) f32x4 *LdsF32x4;
+typedef const __attribute__((address_space(3))) float *LdsF32;
+typedef __attribute__((address_space(3))) uint8_t *LdsU8;
+
+struct Tiling {
+    int64_t n_tiles, tiles; // of the result
+    int64_t per_split;      // blocks of K of one split
+    int splits;
+    int64_t part_ld;        // row length of the partial results (splits > 1)
+};
+
+template <int TM, int TN, int WM, int WN, bool W1, bool EXACT, typename OUT>
+__global__ __launch_bounds__(64 * WM * WN) void tiles_kernel(Product p, Tiling g, OUT *C, float *parts)
+{
+    constexpr int kWaves = WM * WN, BM = 16 * TM * WM, BN = 16 * TN * WN, kRows = BM + BN;
+    constexpr uint32_t kStage = kRows * kRowBytes, kScales = 2 * kStage, kScaleStage = kRows * 4;
+    constexpr int kFetches = kRows / 8 / kWaves;
+    static_assert(kRows % (8 * kWaves) == 0 && kRows % 64 == 0 && kRows / 64 <= kWaves && BM % 64 == 0, "whole fetches");
+    __shared__ __attribute__((aligned(1024))) uint8_t smem[kScales + 2 * kScaleStage];
+    const uint32_t lds = (uint32_t)(uintptr_t)(LdsU8)smem;
+
+    const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), row = lane % 16, part = lane / 16;
+    const int wm = wave % WM, wn = wave / WM;
+    // workgroups go round over the eight XCDs: each XCD takes a contiguous range of the tiles
+    const uint32_t wgs = gridDim.x, xcd = blockIdx.x % 8, in_xcd = blockIdx.x / 8, base = wgs / 8, more = wgs % 8;
+    const uint32_t job = xcd * base + min(xcd, more) + in_xcd;
+    const uint32_t split = job / (uint32_t)g.tiles, tile = job - split * (uint32_t)g.tiles;
+    // tiles in bands of eight along the tokens, so that a range of them shares rows of both operands
+    const uint32_t n_tiles = (uint32_t)g.n_tiles, m_tiles = (uint32_t)(g.tiles / g.n_tiles), band = tile / (8 * n_tiles);
+    const uint32_t in_band = tile - band * 8 * n_tiles, height = min(8u, m_tiles - 8 * band);
+    const int64_t m0 = (int64_t)(8 * band + in_band % height) * BM, n0 = (int64_t)(in_band / height) * BN;
+    const int64_t kb0 = split * g.per_split, kb1 = min(kb0 + g.per_split, p.k_blocks);
+
+    const uint8_t *const a_base = p.A + m0 * p.lda, *const w_base = p.W + n0 * p.ldw;
+    const int m_last = (int)min(p.M - 1 - m0, (int64_t)BM - 1), n_last = (int)min(p.N - 1 - n0, (int64_t)BN - 1);
+    uint32_t at[kFetches]; // this lane's offset of each fetch: rows behind the last repeat it
+#pragma unroll
+    for (int j = 0; j < kFetches; ++j) {
+        const int r = 8 * (wave * kFetches + j) + lane / 8; // of the tile: tokens, then features
+        const uint32_t chunk = 16 * ((lane % 8) ^ (lane / 8));
+        at[j] = (r < BM ? (uint32_t)min(r, m_last) * (uint32_t)p.lda : (uint32_t)min(r - BM, n_last) * (uint32_t)p.ldw) + chunk;
+    }
+    const bool a_scales = 64 * wave < BM;
+    const int64_t w_row0 = n0 / p.w_rows;
+    const uint32_t scale_at = 4 * (a_scales ? (uint32_t)min(64 * wave + lane, m_last)
+                                            : (uint32_t)((n0 + min(64 * wave + lane - BM, n_last)) / p.w_rows - w_row0));
+    const float *const scale_base = a_scales ? p.SA + m0 : p.SW + w_row0;
+    const int64_t scale_step = a_scales ? p.ldsa : p.ldsw;
+
+    auto fetch = [&](int64_t kb) {
+        const uint32_t buf = (uint32_t)(kb & 1);
+        const bool last = kb == p.k_blocks - 1;
+#pragma unroll
+        for (int j = 0; j < kFetches; ++j) {
+            const int g8 = wave * kFetches + j;
+            const bool of_a = 8 * g8 < BM;
+            uint32_t off = at[j];
+            if (last) { // chunks behind the row's end repeat its last one
+                const int32_t room = (int32_t)((of_a ? p.lda : p.ldw) - kb * kBlock) - 16;
+                const int32_t chunk = 16 * ((lane % 8) ^ (lane / 8));
+                off -= (uint32_t)max(0, chunk - room);
+            }
+            fetch16((of_a ? a_base : w_base) + kb * kBlock, off, lds + buf * kStage + 1024u * g8);
+        }
+        if (64 * wave < kRows) fetch4(scale_base + kb * scale_step, scale_at, lds + kScales + buf * kScaleStage + 256u * wave);
+    };
+
+    f32x4 acc[TM][TN];
+#pragma unroll
+    for (int i = 0; i < TM; ++i)
+#pragma unroll
+        for (int j = 0; j < TN; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+
+    const uint32_t frag = row * kRowBytes + 16 * ((2 * part) ^ (row % 8));
+    const uint32_t a_at = lds + wm * (16 * TM * kRowBytes) + frag, w_at = lds + BM * kRowBytes + wn * (16 * TN * kRowBytes) + frag;
+    const uint32_t sa_at = lds + kScales + 4 * (wm * 16 * TM + row), sw_at = lds + kScales + 4 * (BM + wn * 16 * TN + 4 * part);
+
+    fetch(kb0);
+    for (int64_t kb = kb0; kb < kb1; ++kb) {
+        const uint32_t buf = (uint32_t)(kb & 1), stage = buf * kStage, scales = buf * kScaleStage;
+        arrived();
+        barrier(); // block kb is there, and nobody reads the other buffer any more
+        if (kb + 1 < kb1) fetch(kb + 1);
+        if ((kb + 1) * kBlock > p.K) { // codes behind K
+            const int keep = (int)(p.K - kb * kBlock);
+            for (uint32_t i = threadIdx.x; i < kRows * 8; i += 64 * kWaves) {
+                const uint32_t r = i / 8, chunk = (i % 8) ^ (r % 8);
+                __attribute__((address_space(3))) uint32_t *w = (__attribute__((address_space(3))) uint32_t *)(lds + stage + 16 * i);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const int left = keep - (int)(16 * chunk + 4 * e);
+                    if (left <= 0) w[e] = 0;
+                    else if (left < 4) w[e] &= (1u << (8 * left)) - 1u;
+                }
+            }
+            barrier();
+        }
+        auto load = [&](uint32_t a) {
+            const u32x4 lo = *(LdsU32x4)a, hi = *(LdsU32x4)(a ^ 16u);
+            return i32x8{(int)lo[0], (int)lo[1], (int)lo[2], (int)lo[3], (int)hi[0], (int)hi[1], (int)hi[2], (int)hi[3]};
+        };
+        i32x8 a[TM];
+        float s[TM];
+        [[maybe_unused]] const float sw = W1 ? 0.f : *(LdsF32)(sw_at + scales);
+#pragma unroll
+        for (int i = 0; i < TM; ++i) {
+            a[i] = load(a_at + stage + 16 * kRowBytes * i);
+            s[i] = *(LdsF32)(sa_at + scales + 64 * i);
+            if constexpr (!W1) s[i] *= sw;
+        }
+        if constexpr (EXACT) {
+            f16x8 aw[TM][4];
+#pragma unroll
+            for (int i = 0; i < TM; ++i)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) aw[i][e] = widened(a[i][2 * e], a[i][2 * e + 1]);
+#pragma unroll
+            for (int j = 0; j < TN; ++j) {
+                const i32x8 w = load(w_at + stage + 16 * kRowBytes * j);
+                [[maybe_unused]] f32x4 s4;
+                if constexpr (W1) s4 = *(LdsF32x4)(sw_at + scales + 64 * j);
+                f16x8 ww[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) ww[e] = widened(w[2 * e], w[2 * e + 1]);
+#pragma unroll
+                for (int i = 0; i < TM; ++i) {
+                    f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) sum = __builtin_amdgcn_mfma_f32_16x16x32_f16(ww[e], aw[i][e], sum, 0, 0, 0);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) acc[i][j][e] = __builtin_fmaf(sum[e], W1 ? s[i] * s4[e] : s[i], acc[i][j][e]);
+                }
+            }
+        } else {
+#pragma unroll
+            for (int j = 0; j < TN; ++j) {
+                const i32x8 w = load(w_at + stage + 16 * kRowBytes * j);
+                [[maybe_unused]] f32x4 s4;
+                if constexpr (W1) s4 = *(LdsF32x4)(sw_at + scales + 64 * j);
+#pragma unroll
+                for (int i = 0; i < TM; ++i) {
+                    const f32x4 sum = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(w, a[i], f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0, 0, 0, 0);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) acc[i][j][e] = __builtin_fmaf(sum[e], W1 ? s[i] * s4[e] : s[i], acc[i][j][e]);
+                }
+            }
+        }
+    }
+
+#pragma unroll
+    for (int i = 0; i < TM; ++i) {
+        const int64_t m = m0 + 16 * (TM * wm + i) + row;
+#pragma unroll
+        for (int j = 0; j < TN; ++j) {
+            const int64_t n = n0 + 16 * (TN * wn + j) + 4 * part;
+            if (m >= p.M || n >= p.N) continue;
+            if (g.splits > 1) store4(parts + ((int64_t)split * p.M + m) * g.part_ld + n, acc[i][j], p.N - n);
+            else store4(C + m * p.ldc + n, acc[i][j], p.N - n);
+        }
+    }
+}
+
+// The partial results of the splits, added in their order.
+template <typename OUT>
+__global__ __launch_bounds__(256) void join_kernel(const float *parts, int splits, int64_t part_ld, OUT *C, int64_t ldc, int64_t M, int64_t N)
+{
+    const int64_t row_units = part_ld / 4, units = M * row_units, step = M * part_ld;
+    for (int64_t u = (int64_t)blockIdx.x * 256 + threadIdx.x; u < units; u += (int64_t)gridDim.x * 256) {
+        const int64_t m = u / row_units, n = 4 * (u - m * row_units);
+        const float *q = parts + m * part_ld + n;
+        f32x4 sum = *reinterpret_cast<const f32x4 *>(q);
+        for (int i = 1; i < splits; ++i) sum += *reinterpret_cast<const f32x4 *>(q + i * step);
+        store4(C + m * ldc + n, sum, N - n);
+    }
+}
+
+template <int TM, int TN, int WM, int WN, bool EXACT, typename OUT>
+int run_tiles(const Product &p, OUT *C, void *workspace, size_t workspace_bytes, hipStream_t s)
+{
+    constexpr int BM = 16 * TM * WM, BN = 16 * TN * WN;
+    Tiling g;
+    g.n_tiles = ceil_div(p.N, BN);
+    g.tiles = g.n_tiles * ceil_div(p.M, BM);
+    if (g.tiles > kMaxTiles) return ZS_ERR_SHAPE;
+    g.part_ld = (p.N + 3) / 4 * 4;
+    const int64_t cus = zs_compute_units();
+    int64_t splits = g.tiles >= cus ? 1 : cus / g.tiles;
+    splits = std::min(splits, p.k_blocks / 4); // at least four blocks each
+    splits = std::min(splits, workspace ? (int64_t)(workspace_bytes / (4 * (size_t)p.M * (size_t)g.part_ld)) : 0);
+    g.per_split = ceil_div(p.k_blocks, splits > 1 ? splits : 1);
+    g.splits = (int)ceil_div(p.k_blocks, g.per_split);
+    float *parts = static_cast<float *>(workspace);
+    const dim3 grid((unsigned)(g.tiles * g.splits)), wg(64 * WM * WN);
+    if (p.w_rows == 1) hipLaunchKernelGGL((tiles_kernel<TM, TN, WM, WN, true, EXACT, OUT>), grid, wg, 0, s, p, g, C, parts);
+    else hipLaunchKernelGGL((tiles_kernel<TM, TN, WM, WN, false, EXACT, OUT>), grid, wg, 0, s, p, g, C, parts);
+    if (g.splits > 1)
+        hipLaunchKernelGGL(join_kernel<OUT>, dim3(grid_for(ceil_div(p.M * g.part_ld / 4, 256))), dim3(256), 0, s, parts, g.splits, g.part_ld, C,
+                           p.ldc, p.M, p.N);
+    return launched();
+}
+
 template <typename OUT>
 int run(const uint8_t *A, int64_t lda, const float *SA, int64_t ldsa, const uint8_t *W, int64_t ldw, const float *SW, int64_t ldsw, int w_rows,
-        OUT *C, int64_t ldc, int64_t M, int64_t N, int64_t K, void *workspace, size_t, void *hip_stream)
+        OUT *C, int64_t ldc, int64_t M, int64_t N, int64_t K, void *workspace, size_t workspace_bytes, void *hip_stream)
 {
     if (!A || !SA || !W || !SW || !C) return ZS_ERR_ARG;
     if (!aligned(A, 16) || !aligned(W, 16) || !aligned(C, 16) || !aligned(SA, 4) || !aligned(SW, 4) || !aligned(workspace, 256)) return ZS_ERR_ARG;
     if (w_rows != 1 && w_rows != kBlock) return ZS_ERR_CONFIG;
     if (M < 1 || N < 1 || K < 1 || M > INT32_MAX || N > INT32_MAX || K > INT32_MAX) return ZS_ERR_SHAPE;
     if (lda < K || lda % 16 || ldw < K || ldw % 16 || ldc < N || ldc % 4 || ldsa < M || ldsw < ceil_div(N, w_rows)) return ZS_ERR_SHAPE;
+    if (lda > kMaxLd || ldw > kMaxLd) return ZS_ERR_SHAPE; // offsets inside a tile are 32 bits wide
     const Product p = {A, W, SA, SW, lda, ldsa, ldw, ldsw, ldc, M, N, K, ceil_div(K, kBlock), w_rows};
+    hipStream_t stream = static_cast<hipStream_t>(hip_stream);
+    if (M > 64) {
+        constexpr bool kExact = std::is_same_v<OUT, float>;
+        if constexpr (kExact) return run_tiles<4, 4, 4, 2, true>(p, C, workspace, workspace_bytes, stream);
+        else return run_tiles<4, 8, 4, 2, false>(p, C, workspace, workspace_bytes, stream);
+    }
     const int64_t n_tiles = ceil_div(N, 16), tiles = n_tiles * ceil_div(M, 16);
-    hipLaunchKernelGGL(product_kernel<OUT>, dim3(grid_for(ceil_div(tiles, 4))), dim3(256), 0, static_cast<hipStream_t>(hip_stream), p, C, n_tiles,
-                       tiles);
+    hipLaunchKernelGGL(product_kernel<OUT>, dim3(grid_for(ceil_div(tiles, 4))), dim3(256), 0, stream, p, C, n_tiles, tiles);
     return launched();
 }
 
