@@ -22,41 +22,14 @@ struct Product {
     int w_rows;
 };
 
-// 32 codes of one row from column k on, as an operand of the matrix instruction; those behind K are zero.
-__device__ __forceinline__ i32x8 codes32(const uint8_t *row, int64_t k, int64_t K)
-{
-    u32x4 lo = {0, 0, 0, 0}, hi = {0, 0, 0, 0};
-    if (k < K) lo = *reinterpret_cast<const u32x4 *>(row + k);
-    if (k + 16 < K) hi = *reinterpret_cast<const u32x4 *>(row + k + 16);
-    i32x8 v;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const int64_t left = K - (k + 4 * i); // of this word's codes
-        const uint32_t keep = left >= 4 ? ~0u : left <= 0 ? 0u : (1u << (8 * left)) - 1u;
-        v[i] = (int)((i < 4 ? lo[i] : hi[i - 4]) & keep);
-    }
-    return v;
-}
-
-// A block of 128 along K for 16 rows of W (first operand) and of A.  The codes are widened to FP16, which holds every
-// one of them exactly, and so are their products and the FP32 sums of v_mfma_f32_16x16x32_f16 up to FP32's
-// rounding.  (The 8-bit matrix instructions cut each product at 2^-13 of the largest of its group of eight.)  All
-// lanes take their codes in the same order, so which of them meet in one of the four instructions does not matter.
+// Eight codes as FP16 numbers, which hold every one of them exactly; v_mfma_f32_16x16x32_f16 then sums whole products in
+// FP32.  (The 8-bit matrix instructions cut each product at 2^-13 of the largest of its group of eight.)
 __device__ __forceinline__ f16x8 widened(uint32_t lo, uint32_t hi)
 {
     const f16x2 a = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, 1.f, false), b = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, 1.f, true);
     const f16x2 c = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, 1.f, false), d = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, 1.f, true);
     return f16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
 }
-__device__ __forceinline__ f32x4 multiply(i32x8 w, i32x8 a)
-{
-    f32x4 sum = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-    for (int i = 0; i < 8; i += 2)
-        sum = __builtin_amdgcn_mfma_f32_16x16x32_f16(widened(w[i], w[i + 1]), widened(a[i], a[i + 1]), sum, 0, 0, 0);
-    return sum;
-}
-
 __device__ __forceinline__ void store4(float *p, f32x4 v, int64_t left)
 {
     if (left >= 4) {
@@ -76,24 +49,128 @@ __device__ __forceinline__ void store4(uint16_t *p, f32x4 v, int64_t left)
         if (i < left) p[i] = bf16_bits(v[i]);
 }
 
-// A wave computes 16 features x 16 tokens.  W is the first operand, so a lane holds four features of one token.
-template <typename OUT>
-__global__ __launch_bounds__(256) void product_kernel(Product p, OUT *C, int64_t n_tiles, int64_t tiles)
+// ---- few tokens: the weights are read once ----------------------------------------------------
+// A workgroup computes 16 RT features x 16 MT tokens; its NW waves take the blocks of K in turn, each with D blocks
+// requested ahead, and add their sums up in LDS, always in the same order.  W is the first operand, so a lane
+// holds four features of one token.  A lane takes the chunks of 16 bytes `part` and `part` + 4 of its row, so that a
+// load covers 64 contiguous bytes of sixteen rows.
+template <int MT, int RT, int NW, int D, bool W1, typename OUT>
+__global__ __launch_bounds__(64 * NW) void stream_kernel(Product p, OUT *C)
 {
-    const int lane = threadIdx.x % 64, row = lane % 16, part = lane / 16;
-    for (int64_t t = (int64_t)blockIdx.x * 4 + threadIdx.x / 64; t < tiles; t += (int64_t)gridDim.x * 4) {
-        const int64_t mt = t / n_tiles, n0 = 16 * (t - mt * n_tiles), m = 16 * mt + row, n = n0 + 4 * part;
-        const int64_t am = min(m, p.M - 1), wn = min(n0 + row, p.N - 1);
-        f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-        for (int64_t b = 0; b < p.k_blocks; ++b) {
-            const int64_t k = b * kBlock + 32 * part;
-            const f32x4 sum = multiply(codes32(p.W + wn * p.ldw, k, p.K), codes32(p.A + am * p.lda, k, p.K));
-            const float sa = p.SA[b * p.ldsa + am];
+    constexpr int kTiles = MT * RT;
+    __shared__ f32x4 sums[NW][kTiles][64];
+    const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), row = lane % 16, part = lane / 16;
+    const int64_t n0 = (int64_t)blockIdx.x * (16 * RT), m0 = (int64_t)blockIdx.y * (16 * MT);
+    const int m_last = (int)min(p.M - 1 - m0, (int64_t)16 * MT - 1), n_last = (int)min(p.N - 1 - n0, (int64_t)16 * RT - 1);
+    const uint8_t *const a_base = p.A + m0 * p.lda, *const w_base = p.W + n0 * p.ldw;
+    const float *const sa_base = p.SA + m0, *const sw_base = p.SW + n0 / p.w_rows;
+    uint32_t a_row[MT], w_row[RT];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) acc[i] += sum[i] * (sa * p.SW[b * p.ldsw + min(n + i, p.N - 1) / p.w_rows]);
+    for (int i = 0; i < MT; ++i) a_row[i] = (uint32_t)min(16 * i + row, m_last);
+#pragma unroll
+    for (int j = 0; j < RT; ++j) w_row[j] = (uint32_t)min(16 * j + row, n_last) * (uint32_t)p.ldw;
+
+    struct Block {
+        u32x4 w[RT][2], a[MT][2];
+        float sa[MT];
+        f32x4 sw[W1 ? RT : 1];
+    };
+    auto load = [&](Block &b, int64_t kb) {
+        const uint32_t k = (uint32_t)kb * kBlock;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) { // (chunks behind a row's end repeat its last one)
+            const uint32_t w_k = min(k + 16 * part + 64 * h, (uint32_t)p.ldw - 16), a_k = min(k + 16 * part + 64 * h, (uint32_t)p.lda - 16);
+#pragma unroll
+            for (int j = 0; j < RT; ++j) b.w[j][h] = __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(w_base + (w_row[j] + w_k)));
+#pragma unroll
+            for (int i = 0; i < MT; ++i) b.a[i][h] = *reinterpret_cast<const u32x4 *>(a_base + (a_row[i] * (uint32_t)p.lda + a_k));
         }
-        if (m < p.M && n < p.N) store4(C + m * p.ldc + n, acc, p.N - n);
+#pragma unroll
+        for (int i = 0; i < MT; ++i) b.sa[i] = sa_base[kb * p.ldsa + a_row[i]];
+        if constexpr (W1) {
+#pragma unroll
+            for (int j = 0; j < RT; ++j)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) b.sw[j][e] = sw_base[kb * p.ldsw + min(16 * j + 4 * part + e, n_last)];
+        } else {
+            b.sw[0][0] = sw_base[kb * p.ldsw];
+        }
+    };
+    f32x4 acc[MT][RT];
+#pragma unroll
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int j = 0; j < RT; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    auto multiply = [&](Block &b, int64_t kb) {
+        if ((kb + 1) * kBlock > p.K) { // codes behind K
+            const int keep = (int)(p.K - kb * kBlock);
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const int left = keep - (16 * part + 64 * h + 4 * e);
+                    const uint32_t mask = left >= 4 ? ~0u : left <= 0 ? 0u : (1u << (8 * left)) - 1u;
+#pragma unroll
+                    for (int j = 0; j < RT; ++j) b.w[j][h][e] &= mask;
+#pragma unroll
+                    for (int i = 0; i < MT; ++i) b.a[i][h][e] &= mask;
+                }
+        }
+        f16x8 a[MT][4];
+#pragma unroll
+        for (int i = 0; i < MT; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) a[i][e] = widened(b.a[i][e / 2][2 * (e % 2)], b.a[i][e / 2][2 * (e % 2) + 1]);
+#pragma unroll
+        for (int j = 0; j < RT; ++j) {
+            f16x8 w[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) w[e] = widened(b.w[j][e / 2][2 * (e % 2)], b.w[j][e / 2][2 * (e % 2) + 1]);
+#pragma unroll
+            for (int i = 0; i < MT; ++i) {
+                f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int e = 0; e < 4; ++e) sum = __builtin_amdgcn_mfma_f32_16x16x32_f16(w[e], a[i][e], sum, 0, 0, 0);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) acc[i][j][e] = __builtin_fmaf(sum[e], b.sa[i] * (W1 ? b.sw[W1 ? j : 0][e] : b.sw[0][0]), acc[i][j][e]);
+            }
+        }
+    };
+
+    Block b[D];
+#pragma unroll
+    for (int d = 0; d < D; ++d)
+        if (wave + d * NW < p.k_blocks) load(b[d], wave + d * NW);
+    for (int64_t kb = wave; kb < p.k_blocks; kb += D * NW)
+#pragma unroll
+        for (int d = 0; d < D; ++d) {
+            const int64_t now = kb + d * NW, next = now + D * NW;
+            if (now < p.k_blocks) multiply(b[d], now);
+            if (next < p.k_blocks) load(b[d], next);
+        }
+
+#pragma unroll
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int j = 0; j < RT; ++j) sums[wave][i * RT + j][lane] = acc[i][j];
+    __syncthreads();
+    for (int t = wave; t < kTiles; t += NW) {
+        f32x4 sum = sums[0][t][lane];
+#pragma unroll
+        for (int w = 1; w < NW; ++w) sum += sums[w][t][lane];
+        const int64_t m = m0 + 16 * (t / RT) + row, n = n0 + 16 * (t % RT) + 4 * part;
+        if (m < p.M && n < p.N) store4(C + m * p.ldc + n, sum, p.N - n);
     }
+}
+
+template <int MT, int RT, int NW, int D, typename OUT>
+int run_stream(const Product &p, OUT *C, hipStream_t s)
+{
+    const dim3 grid((unsigned)ceil_div(p.N, 16 * RT), (unsigned)ceil_div(p.M, 16 * MT)), wg(64 * NW);
+    if (grid.x > kMaxTiles) return ZS_ERR_SHAPE;
+    if (p.w_rows == 1) hipLaunchKernelGGL((stream_kernel<MT, RT, NW, D, true, OUT>), grid, wg, 0, s, p, C);
+    else hipLaunchKernelGGL((stream_kernel<MT, RT, NW, D, false, OUT>), grid, wg, 0, s, p, C);
+    return launched();
 }
 
 // ---- tiles through LDS ---------------------------------------------------------------------
@@ -332,14 +409,14 @@ int run(const uint8_t *A, int64_t lda, const float *SA, int64_t ldsa, const uint
     if (lda > kMaxLd || ldw > kMaxLd) return ZS_ERR_SHAPE; // offsets inside a tile are 32 bits wide
     const Product p = {A, W, SA, SW, lda, ldsa, ldw, ldsw, ldc, M, N, K, ceil_div(K, kBlock), w_rows};
     hipStream_t stream = static_cast<hipStream_t>(hip_stream);
-    if (M > 64) {
+    if (M > 32) {
+        if (M <= 64) return run_tiles<4, 2, 1, 4, true>(p, C, workspace, workspace_bytes, stream);
         constexpr bool kExact = std::is_same_v<OUT, float>;
         if constexpr (kExact) return run_tiles<4, 4, 4, 2, true>(p, C, workspace, workspace_bytes, stream);
         else return run_tiles<4, 8, 4, 2, false>(p, C, workspace, workspace_bytes, stream);
     }
-    const int64_t n_tiles = ceil_div(N, 16), tiles = n_tiles * ceil_div(M, 16);
-    hipLaunchKernelGGL(product_kernel<OUT>, dim3(grid_for(ceil_div(tiles, 4))), dim3(256), 0, stream, p, C, n_tiles, tiles);
-    return launched();
+    if (M > 16) return run_stream<2, 1, 8, 4>(p, C, stream);
+    return run_stream<1, 1, 8, 4>(p, C, stream);
 }
 
 } // namespace
