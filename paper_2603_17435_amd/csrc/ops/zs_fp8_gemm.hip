@@ -4,6 +4,7 @@
 #include "zs_ops.h"
 
 #include <algorithm>
+#include <cmath>
 #include <type_traits>
 
 using namespace zs_ops;
@@ -30,6 +31,14 @@ __device__ __forceinline__ f16x8 widened(uint32_t lo, uint32_t hi)
     const f16x2 c = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, 1.f, false), d = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, 1.f, true);
     return f16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
 }
+__device__ __forceinline__ i32x8 joined(u32x4 lo, u32x4 hi)
+{
+    return i32x8{(int)lo[0], (int)lo[1], (int)lo[2], (int)lo[3], (int)hi[0], (int)hi[1], (int)hi[2], (int)hi[3]};
+}
+
+// Mask of a word of four codes of which `left` lie before K.
+__device__ __forceinline__ uint32_t kept(int left) { return left >= 4 ? ~0u : left <= 0 ? 0u : (1u << (8 * left)) - 1u; }
+
 __device__ __forceinline__ void store4(float *p, f32x4 v, int64_t left)
 {
     if (left >= 4) {
@@ -50,137 +59,160 @@ __device__ __forceinline__ void store4(uint16_t *p, f32x4 v, int64_t left)
 }
 
 // ---- few tokens: the weights are read once ----------------------------------------------------
-// A workgroup computes 16 RT features x 16 MT tokens; its NW waves take the blocks of K in turn, each with D blocks
-// requested ahead, and add their sums up in LDS, always in the same order.  W is the first operand, so a lane
-// holds four features of one token.  A lane takes the chunks of 16 bytes `part` and `part` + 4 of its row, so that a
-// load covers 64 contiguous bytes of sixteen rows.
-template <int MT, int RT, int NW, int D, bool W1, typename OUT>
-__global__ __launch_bounds__(64 * NW) void stream_kernel(Product p, OUT *C)
+// A workgroup keeps all M <= 16 MT tokens' codes of a slice of K in LDS and multiplies them by one tile of 16 features after
+// another.  Its NW waves share a tile's blocks of 128 along K and add their sums up in LDS, always in the same order.
+// Each wave requests its blocks of W, of this tile and the next ones, D ahead, straight into operand registers: a lane
+// takes the chunks of 16 bytes `part` and `part` + 4 of its row, so that a load covers 64 contiguous bytes
+// of sixteen rows.  W is the first operand, so a lane holds four features of one token.
+constexpr size_t kLds = 160 * 1024;
+constexpr size_t stream_sums(int mt, int waves) { return (size_t)2 * waves * mt * 1024; }
+constexpr size_t stream_block(int rows) { return (size_t)rows * (kBlock + 4); } // a block's codes and scales
+
+struct Stream {
+    int64_t n_tiles;
+    int64_t per_slice; // blocks of K in a slice
+    int slices, wgs;   // workgroups of a slice
+    int64_t part_ld;   // row length of the partial results (slices > 1)
+};
+
+template <int MT, int NW, int D, bool W1, typename OUT>
+__global__ __launch_bounds__(64 * NW) void stream_kernel(Product p, Stream g, OUT *C, float *parts)
 {
-    constexpr int kTiles = MT * RT;
-    __shared__ f32x4 sums[NW][kTiles][64];
+    extern __shared__ __attribute__((aligned(16))) uint8_t smem[];
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), row = lane % 16, part = lane / 16;
-    const int64_t n0 = (int64_t)blockIdx.x * (16 * RT), m0 = (int64_t)blockIdx.y * (16 * MT);
-    const int m_last = (int)min(p.M - 1 - m0, (int64_t)16 * MT - 1), n_last = (int)min(p.N - 1 - n0, (int64_t)16 * RT - 1);
-    const uint8_t *const a_base = p.A + m0 * p.lda, *const w_base = p.W + n0 * p.ldw;
-    const float *const sa_base = p.SA + m0, *const sw_base = p.SW + n0 / p.w_rows;
-    uint32_t a_row[MT], w_row[RT];
-#pragma unroll
-    for (int i = 0; i < MT; ++i) a_row[i] = (uint32_t)min(16 * i + row, m_last);
-#pragma unroll
-    for (int j = 0; j < RT; ++j) w_row[j] = (uint32_t)min(16 * j + row, n_last) * (uint32_t)p.ldw;
+    const int slice = blockIdx.x / g.wgs, first = blockIdx.x - slice * g.wgs;
+    const int64_t kb0 = slice * g.per_slice;
+    const int blocks = (int)min(g.per_slice, p.k_blocks - kb0), rows = (int)p.M;
+    const int tiles = (int)((g.n_tiles - first + g.wgs - 1) / g.wgs); // of this workgroup: first, first + wgs, ...
+    f32x4 *const sums = reinterpret_cast<f32x4 *>(smem);              // [2][NW][MT][64]
+    uint8_t *const codes = smem + stream_sums(MT, NW);               // [blocks][rows][128], chunk c of a row at c ^ (row % 8)
+    float *const scales = reinterpret_cast<float *>(codes + (size_t)blocks * rows * kBlock); // [blocks][rows]
 
     struct Block {
-        u32x4 w[RT][2], a[MT][2];
-        float sa[MT];
-        f32x4 sw[W1 ? RT : 1];
+        u32x4 w[2];
+        f32x4 sw;
     };
-    auto load = [&](Block &b, int64_t kb) {
-        const uint32_t k = (uint32_t)kb * kBlock;
+    const int per_tile = (blocks - wave + NW - 1) / NW; // blocks of this wave in a tile: wave, wave + NW, ...
+    Block b[D];
+    int at_tile = 0, at_block = 0; // of the next request
+    auto request = [&](Block &to) {
+        if (at_tile >= tiles) return;
+        const int64_t n0 = 16 * (first + (int64_t)at_tile * g.wgs), kb = kb0 + wave + at_block * NW;
+        const int n_last = (int)min(p.N - 1 - n0, (int64_t)15);
+        const uint8_t *base = p.W + n0 * p.ldw + kb * kBlock;
+        const uint32_t room = (uint32_t)min(p.ldw - kb * kBlock - 16, (int64_t)112), at = (uint32_t)min(row, n_last) * (uint32_t)p.ldw;
 #pragma unroll
-        for (int h = 0; h < 2; ++h) { // (chunks behind a row's end repeat its last one)
-            const uint32_t w_k = min(k + 16 * part + 64 * h, (uint32_t)p.ldw - 16), a_k = min(k + 16 * part + 64 * h, (uint32_t)p.lda - 16);
-#pragma unroll
-            for (int j = 0; j < RT; ++j) b.w[j][h] = __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(w_base + (w_row[j] + w_k)));
-#pragma unroll
-            for (int i = 0; i < MT; ++i) b.a[i][h] = *reinterpret_cast<const u32x4 *>(a_base + (a_row[i] * (uint32_t)p.lda + a_k));
-        }
-#pragma unroll
-        for (int i = 0; i < MT; ++i) b.sa[i] = sa_base[kb * p.ldsa + a_row[i]];
+        for (int h = 0; h < 2; ++h) // (chunks behind the row's end repeat its last one)
+            to.w[h] = __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(base + (at + min((uint32_t)(16 * part + 64 * h), room))));
+        const float *sw = p.SW + kb * p.ldsw;
         if constexpr (W1) {
 #pragma unroll
-            for (int j = 0; j < RT; ++j)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) b.sw[j][e] = sw_base[kb * p.ldsw + min(16 * j + 4 * part + e, n_last)];
+            for (int e = 0; e < 4; ++e) to.sw[e] = sw[n0 + min(4 * part + e, n_last)];
         } else {
-            b.sw[0][0] = sw_base[kb * p.ldsw];
+            to.sw[0] = sw[n0 / kBlock];
+        }
+        if (++at_block >= per_tile) {
+            at_block = 0;
+            ++at_tile;
         }
     };
-    f32x4 acc[MT][RT];
+    if (per_tile > 0)
 #pragma unroll
-    for (int i = 0; i < MT; ++i)
+        for (int d = 0; d < D; ++d) request(b[d]);
+
+    for (int i = threadIdx.x; i < blocks * rows * 8; i += 64 * NW) {
+        const int chunk = i % 8, r = i / 8 % rows, kb = i / 8 / rows;
+        const int64_t k = (kb0 + kb) * kBlock + 16 * chunk;
+        u32x4 v = {0, 0, 0, 0};
+        if (k < p.K) v = *reinterpret_cast<const u32x4 *>(p.A + r * p.lda + k);
+        if (k + 16 > p.K) {
 #pragma unroll
-        for (int j = 0; j < RT; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-    auto multiply = [&](Block &b, int64_t kb) {
+            for (int e = 0; e < 4; ++e) v[e] &= kept((int)(p.K - (k + 4 * e)));
+        }
+        *reinterpret_cast<u32x4 *>(codes + (size_t)(kb * rows + r) * kBlock + 16 * (chunk ^ (r % 8))) = v;
+    }
+    for (int i = threadIdx.x; i < blocks * rows; i += 64 * NW) scales[i] = p.SA[(kb0 + i / rows) * p.ldsa + i % rows];
+    __syncthreads();
+
+    int r[MT];
+#pragma unroll
+    for (int i = 0; i < MT; ++i) r[i] = min(16 * i + row, rows - 1);
+    f32x4 acc[MT];
+    auto clear = [&] {
+#pragma unroll
+        for (int i = 0; i < MT; ++i) acc[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+    };
+    clear();
+    auto multiply = [&](Block &v, int block) {
+        const int64_t kb = kb0 + block;
         if ((kb + 1) * kBlock > p.K) { // codes behind K
-            const int keep = (int)(p.K - kb * kBlock);
 #pragma unroll
             for (int h = 0; h < 2; ++h)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const int left = keep - (16 * part + 64 * h + 4 * e);
-                    const uint32_t mask = left >= 4 ? ~0u : left <= 0 ? 0u : (1u << (8 * left)) - 1u;
-#pragma unroll
-                    for (int j = 0; j < RT; ++j) b.w[j][h][e] &= mask;
-#pragma unroll
-                    for (int i = 0; i < MT; ++i) b.a[i][h][e] &= mask;
-                }
+                for (int e = 0; e < 4; ++e) v.w[h][e] &= kept((int)(p.K - (kb * kBlock + 16 * part + 64 * h + 4 * e)));
         }
-        f16x8 a[MT][4];
+        f16x8 w[4];
 #pragma unroll
-        for (int i = 0; i < MT; ++i)
+        for (int e = 0; e < 4; ++e) w[e] = widened(v.w[e / 2][2 * (e % 2)], v.w[e / 2][2 * (e % 2) + 1]);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) a[i][e] = widened(b.a[i][e / 2][2 * (e % 2)], b.a[i][e / 2][2 * (e % 2) + 1]);
+        for (int i = 0; i < MT; ++i) {
+            const uint8_t *c = codes + (size_t)(block * rows + r[i]) * kBlock;
+            const u32x4 a[2] = {*reinterpret_cast<const u32x4 *>(c + 16 * (part ^ (r[i] % 8))),
+                                *reinterpret_cast<const u32x4 *>(c + 16 * ((part + 4) ^ (r[i] % 8)))};
+            f32x4 sum = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int j = 0; j < RT; ++j) {
-            f16x8 w[4];
+            for (int e = 0; e < 4; ++e)
+                sum = __builtin_amdgcn_mfma_f32_16x16x32_f16(w[e], widened(a[e / 2][2 * (e % 2)], a[e / 2][2 * (e % 2) + 1]), sum, 0, 0, 0);
+            const float sa = scales[block * rows + r[i]];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) w[e] = widened(b.w[j][e / 2][2 * (e % 2)], b.w[j][e / 2][2 * (e % 2) + 1]);
-#pragma unroll
-            for (int i = 0; i < MT; ++i) {
-                f32x4 sum = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                for (int e = 0; e < 4; ++e) sum = __builtin_amdgcn_mfma_f32_16x16x32_f16(w[e], a[i][e], sum, 0, 0, 0);
-#pragma unroll
-                for (int e = 0; e < 4; ++e) acc[i][j][e] = __builtin_fmaf(sum[e], b.sa[i] * (W1 ? b.sw[W1 ? j : 0][e] : b.sw[0][0]), acc[i][j][e]);
-            }
+            for (int e = 0; e < 4; ++e) acc[i][e] = __builtin_fmaf(sum[e], sa * v.sw[W1 ? e : 0], acc[i][e]);
         }
     };
-
-    Block b[D];
+    int tile = 0, block = 0;
+    auto finish = [&] { // the tile is done: its sums of all waves, added by one of them
+        f32x4 *const mine = sums + (tile % 2) * (NW * MT * 64);
 #pragma unroll
-    for (int d = 0; d < D; ++d)
-        if (wave + d * NW < p.k_blocks) load(b[d], wave + d * NW);
-    for (int64_t kb = wave; kb < p.k_blocks; kb += D * NW)
+        for (int i = 0; i < MT; ++i) mine[(wave * MT + i) * 64 + lane] = acc[i];
+        __syncthreads();
+        for (int i = 0; i < MT; ++i) {
+            if ((tile * MT + i) % NW != wave) continue;
+            f32x4 sum = mine[i * 64 + lane];
+#pragma unroll
+            for (int w = 1; w < NW; ++w) sum += mine[(w * MT + i) * 64 + lane];
+            const int64_t m = 16 * i + row, n = 16 * (first + (int64_t)tile * g.wgs) + 4 * part;
+            if (m < p.M && n < p.N) {
+                if (g.slices > 1) store4(parts + ((int64_t)slice * p.M + m) * g.part_ld + n, sum, p.N - n);
+                else store4(C + m * p.ldc + n, sum, p.N - n);
+            }
+        }
+        clear();
+        block = 0;
+        ++tile;
+    };
+    if (per_tile <= 0) { // fewer blocks than waves: only the barriers and the sums
+        while (tile < tiles) finish();
+        return;
+    }
+    while (tile < tiles) {
 #pragma unroll
         for (int d = 0; d < D; ++d) {
-            const int64_t now = kb + d * NW, next = now + D * NW;
-            if (now < p.k_blocks) multiply(b[d], now);
-            if (next < p.k_blocks) load(b[d], next);
+            if (tile < tiles) {
+                multiply(b[d], wave + block * NW);
+                request(b[d]);
+                if (++block == per_tile) finish();
+            }
         }
-
-#pragma unroll
-    for (int i = 0; i < MT; ++i)
-#pragma unroll
-        for (int j = 0; j < RT; ++j) sums[wave][i * RT + j][lane] = acc[i][j];
-    __syncthreads();
-    for (int t = wave; t < kTiles; t += NW) {
-        f32x4 sum = sums[0][t][lane];
-#pragma unroll
-        for (int w = 1; w < NW; ++w) sum += sums[w][t][lane];
-        const int64_t m = m0 + 16 * (t / RT) + row, n = n0 + 16 * (t % RT) + 4 * part;
-        if (m < p.M && n < p.N) store4(C + m * p.ldc + n, sum, p.N - n);
     }
-}
-
-template <int MT, int RT, int NW, int D, typename OUT>
-int run_stream(const Product &p, OUT *C, hipStream_t s)
-{
-    const dim3 grid((unsigned)ceil_div(p.N, 16 * RT), (unsigned)ceil_div(p.M, 16 * MT)), wg(64 * NW);
-    if (grid.x > kMaxTiles) return ZS_ERR_SHAPE;
-    if (p.w_rows == 1) hipLaunchKernelGGL((stream_kernel<MT, RT, NW, D, true, OUT>), grid, wg, 0, s, p, C);
-    else hipLaunchKernelGGL((stream_kernel<MT, RT, NW, D, false, OUT>), grid, wg, 0, s, p, C);
-    return launched();
 }
 
 // ---- tiles through LDS ---------------------------------------------------------------------
 // A workgroup of WM x WN waves computes (16 TM WM) tokens x (16 TN WN) features over the blocks [kb0, kb1) of K.  Each
-// block's codes and scales go from memory straight to LDS (two buffers: block b + 1 is under way while b is
-// multiplied, one barrier a block).  A row's eight chunks of 16 bytes lie in the order chunk ^ (row % 8), so that
+// block's codes and scales go from memory straight to LDS; STAGES - 1 blocks are under way while one is
+// multiplied, and there is one barrier a block.  A row's eight chunks of 16 bytes lie in the order chunk ^ (row % 8), so that
 // the sixteen rows of an operand are read without bank conflicts.
 constexpr int kRowBytes = 128;
 
-// 64 lanes x 16 (or 4) bytes from base + at to the 1 KB (256 bytes) of LDS at `to`.  Not tracked by the compiler: arrived().
+// 64 lanes x 16 (or 4) bytes from base + at to the 1 KB (256 bytes) of LDS at `to`.  Not tracked by the compiler: arrived() waits for them.
 __device__ __forceinline__ void fetch16(const void *base, uint32_t at, uint32_t to)
 {
     asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(at), "s"(base), "s"(to) : "memory", "m0");
@@ -189,7 +221,12 @@ __device__ __forceinline__ void fetch4(const void *base, uint32_t at, uint32_t t
 {
     asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dword %0, %1" ::"v"(at), "s"(base), "s"(to) : "memory", "m0");
 }
-__device__ __forceinline__ void arrived() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+template <int LEFT> // all fetches of this wave but the youngest LEFT
+__device__ __forceinline__ void arrived()
+{
+    static_assert(LEFT < 64, "vmcnt is a 6-bit counter");
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(LEFT) : "memory");
+}
 __device__ __forceinline__ void barrier()
 {
     asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
@@ -207,27 +244,41 @@ struct Tiling {
     int64_t part_ld;        // row length of the partial results (splits > 1)
 };
 
-template <int TM, int TN, int WM, int WN, bool W1, bool EXACT, typename OUT>
+// The tile that a workgroup computes.  Workgroups go round over the eight XCDs, each with an L2 of its own: an XCD
+// takes a contiguous range of the tiles, which lie in bands of eight along the tokens, so that the range shares rows
+// of both operands.
+struct TilePlace {
+    uint32_t split, m, n;
+};
+__device__ __forceinline__ TilePlace place_of(uint32_t wg, uint32_t wgs, const Tiling &g)
+{
+    const uint32_t xcd = wg % 8, job = xcd * (wgs / 8) + min(xcd, wgs % 8) + wg / 8;
+    const uint32_t tiles = (uint32_t)g.tiles, n_tiles = (uint32_t)g.n_tiles, m_tiles = tiles / n_tiles;
+    TilePlace at;
+    at.split = job / tiles;
+    const uint32_t tile = job - at.split * tiles, band = tile / (8 * n_tiles), in_band = tile - band * 8 * n_tiles;
+    const uint32_t height = min(8u, m_tiles - 8 * band);
+    at.m = 8 * band + in_band % height;
+    at.n = in_band / height;
+    return at;
+}
+
+template <int TM, int TN, int WM, int WN, int STAGES, bool W1, bool EXACT, typename OUT>
 __global__ __launch_bounds__(64 * WM * WN) void tiles_kernel(Product p, Tiling g, OUT *C, float *parts)
 {
     constexpr int kWaves = WM * WN, BM = 16 * TM * WM, BN = 16 * TN * WN, kRows = BM + BN;
-    constexpr uint32_t kStage = kRows * kRowBytes, kScales = 2 * kStage, kScaleStage = kRows * 4;
+    constexpr uint32_t kStage = kRows * (kRowBytes + 4), kScales = kRows * kRowBytes;
     constexpr int kFetches = kRows / 8 / kWaves;
     static_assert(kRows % (8 * kWaves) == 0 && kRows % 64 == 0 && kRows / 64 <= kWaves && BM % 64 == 0, "whole fetches");
-    __shared__ __attribute__((aligned(1024))) uint8_t smem[kScales + 2 * kScaleStage];
+    __shared__ __attribute__((aligned(1024))) uint8_t smem[STAGES * kStage];
     const uint32_t lds = (uint32_t)(uintptr_t)(LdsU8)smem;
 
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), row = lane % 16, part = lane / 16;
     const int wm = wave % WM, wn = wave / WM;
-    // workgroups go round over the eight XCDs: each XCD takes a contiguous range of the tiles
-    const uint32_t wgs = gridDim.x, xcd = blockIdx.x % 8, in_xcd = blockIdx.x / 8, base = wgs / 8, more = wgs % 8;
-    const uint32_t job = xcd * base + min(xcd, more) + in_xcd;
-    const uint32_t split = job / (uint32_t)g.tiles, tile = job - split * (uint32_t)g.tiles;
-    // tiles in bands of eight along the tokens, so that a range of them shares rows of both operands
-    const uint32_t n_tiles = (uint32_t)g.n_tiles, m_tiles = (uint32_t)(g.tiles / g.n_tiles), band = tile / (8 * n_tiles);
-    const uint32_t in_band = tile - band * 8 * n_tiles, height = min(8u, m_tiles - 8 * band);
-    const int64_t m0 = (int64_t)(8 * band + in_band % height) * BM, n0 = (int64_t)(in_band / height) * BN;
-    const int64_t kb0 = split * g.per_split, kb1 = min(kb0 + g.per_split, p.k_blocks);
+    const TilePlace place = place_of(blockIdx.x, gridDim.x, g);
+    const uint32_t split = place.split;
+    const int64_t m0 = (int64_t)place.m * BM, n0 = (int64_t)place.n * BN;
+    const int kb0 = (int)(split * (uint32_t)g.per_split), kb1 = min(kb0 + (int)g.per_split, (int)p.k_blocks);
 
     const uint8_t *const a_base = p.A + m0 * p.lda, *const w_base = p.W + n0 * p.ldw;
     const int m_last = (int)min(p.M - 1 - m0, (int64_t)BM - 1), n_last = (int)min(p.N - 1 - n0, (int64_t)BN - 1);
@@ -238,29 +289,29 @@ __global__ __launch_bounds__(64 * WM * WN) void tiles_kernel(Product p, Tiling g
         const uint32_t chunk = 16 * ((lane % 8) ^ (lane / 8));
         at[j] = (r < BM ? (uint32_t)min(r, m_last) * (uint32_t)p.lda : (uint32_t)min(r - BM, n_last) * (uint32_t)p.ldw) + chunk;
     }
-    const bool a_scales = 64 * wave < BM;
+    const int sw_wave = wave % (kRows / 64); // every wave fetches scales, so that all count the same
+    const bool a_scales = 64 * sw_wave < BM;
     const int64_t w_row0 = n0 / p.w_rows;
-    const uint32_t scale_at = 4 * (a_scales ? (uint32_t)min(64 * wave + lane, m_last)
-                                            : (uint32_t)((n0 + min(64 * wave + lane - BM, n_last)) / p.w_rows - w_row0));
+    const uint32_t scale_at = 4 * (a_scales ? (uint32_t)min(64 * sw_wave + lane, m_last)
+                                            : (uint32_t)((n0 + min(64 * sw_wave + lane - BM, n_last)) / p.w_rows - w_row0));
     const float *const scale_base = a_scales ? p.SA + m0 : p.SW + w_row0;
     const int64_t scale_step = a_scales ? p.ldsa : p.ldsw;
 
-    auto fetch = [&](int64_t kb) {
-        const uint32_t buf = (uint32_t)(kb & 1);
-        const bool last = kb == p.k_blocks - 1;
+    const int k_last = (int)p.k_blocks - 1;
+    auto fetch = [&](int kb, uint32_t stage) {
+        if (kb == k_last) { // chunks behind the row's end repeat its last one
+            const int chunk = 16 * ((lane % 8) ^ (lane / 8));
+            const int a_over = max(0, chunk + 16 - (int)(p.lda - (int64_t)kb * kBlock)), w_over = max(0, chunk + 16 - (int)(p.ldw - (int64_t)kb * kBlock));
+#pragma unroll
+            for (int j = 0; j < kFetches; ++j) at[j] -= 8 * (wave * kFetches + j) < BM ? a_over : w_over;
+        }
+        const uint8_t *const a_block = a_base + (int64_t)kb * kBlock, *const w_block = w_base + (int64_t)kb * kBlock;
 #pragma unroll
         for (int j = 0; j < kFetches; ++j) {
             const int g8 = wave * kFetches + j;
-            const bool of_a = 8 * g8 < BM;
-            uint32_t off = at[j];
-            if (last) { // chunks behind the row's end repeat its last one
-                const int32_t room = (int32_t)((of_a ? p.lda : p.ldw) - kb * kBlock) - 16;
-                const int32_t chunk = 16 * ((lane % 8) ^ (lane / 8));
-                off -= (uint32_t)max(0, chunk - room);
-            }
-            fetch16((of_a ? a_base : w_base) + kb * kBlock, off, lds + buf * kStage + 1024u * g8);
+            fetch16(8 * g8 < BM ? a_block : w_block, at[j], lds + stage + 1024u * g8);
         }
-        if (64 * wave < kRows) fetch4(scale_base + kb * scale_step, scale_at, lds + kScales + buf * kScaleStage + 256u * wave);
+        fetch4(scale_base + kb * scale_step, scale_at, lds + stage + kScales + 256u * sw_wave);
     };
 
     f32x4 acc[TM][TN];
@@ -269,78 +320,92 @@ __global__ __launch_bounds__(64 * WM * WN) void tiles_kernel(Product p, Tiling g
 #pragma unroll
         for (int j = 0; j < TN; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
 
-    const uint32_t frag = row * kRowBytes + 16 * ((2 * part) ^ (row % 8));
+    // a lane takes the chunks `part` and `part` + 4 of its row
+    const uint32_t frag = row * kRowBytes + 16 * (part ^ (row % 8));
     const uint32_t a_at = lds + wm * (16 * TM * kRowBytes) + frag, w_at = lds + BM * kRowBytes + wn * (16 * TN * kRowBytes) + frag;
     const uint32_t sa_at = lds + kScales + 4 * (wm * 16 * TM + row), sw_at = lds + kScales + 4 * (BM + wn * 16 * TN + 4 * part);
 
-    fetch(kb0);
-    for (int64_t kb = kb0; kb < kb1; ++kb) {
-        const uint32_t buf = (uint32_t)(kb & 1), stage = buf * kStage, scales = buf * kScaleStage;
-        arrived();
-        barrier(); // block kb is there, and nobody reads the other buffer any more
-        if (kb + 1 < kb1) fetch(kb + 1);
-        if ((kb + 1) * kBlock > p.K) { // codes behind K
-            const int keep = (int)(p.K - kb * kBlock);
+#pragma unroll
+    for (int i = 0; i < STAGES - 1; ++i)
+        if (kb0 + i < kb1) fetch(kb0 + i, i * kStage);
+    uint32_t stage = 0, ahead = (STAGES - 1) * kStage; // where block kb is, and where block kb + STAGES - 1 goes
+    for (int kb = kb0; kb < kb1; ++kb, stage = stage == (STAGES - 1) * kStage ? 0 : stage + kStage,
+             ahead = ahead == (STAGES - 1) * kStage ? 0 : ahead + kStage) {
+        if constexpr (STAGES > 2) {
+            if (kb + STAGES - 2 < kb1) arrived<(STAGES - 2) * (kFetches + 1)>();
+            else arrived<0>(); // (the last blocks: less is under way)
+        } else {
+            arrived<0>();
+        }
+        barrier(); // block kb is there, and nobody reads block kb - 1's buffer any more
+        if (kb + STAGES - 1 < kb1) fetch(kb + STAGES - 1, ahead);
+        if (kb == k_last && p.K % kBlock) { // codes behind K
+            const int keep = (int)(p.K % kBlock);
             for (uint32_t i = threadIdx.x; i < kRows * 8; i += 64 * kWaves) {
                 const uint32_t r = i / 8, chunk = (i % 8) ^ (r % 8);
                 __attribute__((address_space(3))) uint32_t *w = (__attribute__((address_space(3))) uint32_t *)(lds + stage + 16 * i);
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const int left = keep - (int)(16 * chunk + 4 * e);
-                    if (left <= 0) w[e] = 0;
-                    else if (left < 4) w[e] &= (1u << (8 * left)) - 1u;
-                }
+                for (int e = 0; e < 4; ++e) w[e] &= kept(keep - (int)(16 * chunk + 4 * e));
             }
             barrier();
         }
-        auto load = [&](uint32_t a) {
-            const u32x4 lo = *(LdsU32x4)a, hi = *(LdsU32x4)(a ^ 16u);
-            return i32x8{(int)lo[0], (int)lo[1], (int)lo[2], (int)lo[3], (int)hi[0], (int)hi[1], (int)hi[2], (int)hi[3]};
+        const uint32_t a_lo = a_at + stage, a_hi = (a_at ^ 64u) + stage, w_lo = w_at + stage, w_hi = (w_at ^ 64u) + stage;
+        auto codes = [&](uint32_t lo, uint32_t hi, int tile) {
+            return joined(*(LdsU32x4)(lo + 16 * kRowBytes * tile), *(LdsU32x4)(hi + 16 * kRowBytes * tile));
         };
-        i32x8 a[TM];
+        // A sum is scaled and added while the matrix cores work on the next ones.
+        i32x8 a[TM], w[2];
+        f32x4 s4[2];
         float s[TM];
-        [[maybe_unused]] const float sw = W1 ? 0.f : *(LdsF32)(sw_at + scales);
+        w[0] = codes(w_lo, w_hi, 0);
 #pragma unroll
-        for (int i = 0; i < TM; ++i) {
-            a[i] = load(a_at + stage + 16 * kRowBytes * i);
-            s[i] = *(LdsF32)(sa_at + scales + 64 * i);
-            if constexpr (!W1) s[i] *= sw;
-        }
+        for (int i = 0; i < TM; ++i) a[i] = codes(a_lo, a_hi, i);
+        const float sw = W1 ? 1.f : *(LdsF32)(sw_at + stage);
+#pragma unroll
+        for (int i = 0; i < TM; ++i) s[i] = *(LdsF32)(sa_at + stage + 64 * i) * sw;
+        auto add = [&](f32x4 sum, int i, int j) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) acc[i][j][e] = __builtin_fmaf(sum[e], W1 ? s[i] * s4[j % 2][e] : s[i], acc[i][j][e]);
+            asm volatile("" : "+v"(acc[i][j])); // here, and not behind the next barrier
+        };
         if constexpr (EXACT) {
-            f16x8 aw[TM][4];
+            f16x8 aw[TM][4], ww[4];
+            f32x4 sum[2][TM];
 #pragma unroll
             for (int i = 0; i < TM; ++i)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) aw[i][e] = widened(a[i][2 * e], a[i][2 * e + 1]);
 #pragma unroll
-            for (int j = 0; j < TN; ++j) {
-                const i32x8 w = load(w_at + stage + 16 * kRowBytes * j);
-                [[maybe_unused]] f32x4 s4;
-                if constexpr (W1) s4 = *(LdsF32x4)(sw_at + scales + 64 * j);
-                f16x8 ww[4];
+            for (int j = 0; j <= TN; ++j) {
+                if (j < TN) {
 #pragma unroll
-                for (int e = 0; e < 4; ++e) ww[e] = widened(w[2 * e], w[2 * e + 1]);
+                    for (int e = 0; e < 4; ++e) ww[e] = widened(w[j % 2][2 * e], w[j % 2][2 * e + 1]);
+                    if (j + 1 < TN) w[(j + 1) % 2] = codes(w_lo, w_hi, j + 1);
+                    if constexpr (W1) s4[j % 2] = *(LdsF32x4)(sw_at + stage + 64 * j);
 #pragma unroll
-                for (int i = 0; i < TM; ++i) {
-                    f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+                    for (int e = 0; e < 4; ++e)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) sum = __builtin_amdgcn_mfma_f32_16x16x32_f16(ww[e], aw[i][e], sum, 0, 0, 0);
+                        for (int i = 0; i < TM; ++i)
+                            sum[j % 2][i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(ww[e], aw[i][e], e ? sum[j % 2][i] : f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
+                }
+                if (j > 0) {
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) acc[i][j][e] = __builtin_fmaf(sum[e], W1 ? s[i] * s4[e] : s[i], acc[i][j][e]);
+                    for (int i = 0; i < TM; ++i) add(sum[(j + 1) % 2][i], i, j - 1);
                 }
             }
         } else {
+            constexpr int kLag = TM < 3 ? TM : 3; // (w and s4 of a tile are gone when the one after the next is read)
+            f32x4 sum[kLag + 1];
 #pragma unroll
-            for (int j = 0; j < TN; ++j) {
-                const i32x8 w = load(w_at + stage + 16 * kRowBytes * j);
-                [[maybe_unused]] f32x4 s4;
-                if constexpr (W1) s4 = *(LdsF32x4)(sw_at + scales + 64 * j);
-#pragma unroll
-                for (int i = 0; i < TM; ++i) {
-                    const f32x4 sum = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(w, a[i], f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0, 0, 0, 0);
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) acc[i][j][e] = __builtin_fmaf(sum[e], W1 ? s[i] * s4[e] : s[i], acc[i][j][e]);
+            for (int t = 0; t < TM * TN + kLag; ++t) {
+                const int j = t / TM;
+                if (t % TM == 0 && j + 1 < TN) w[(j + 1) % 2] = codes(w_lo, w_hi, j + 1);
+                if constexpr (W1) {
+                    if (t % TM == 0 && j < TN) s4[j % 2] = *(LdsF32x4)(sw_at + stage + 64 * j);
                 }
+                if (t < TM * TN)
+                    sum[t % (kLag + 1)] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(w[j % 2], a[t % TM], f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0, 0, 0, 0);
+                if (t >= kLag) add(sum[(t - kLag) % (kLag + 1)], (t - kLag) % TM, (t - kLag) / TM);
             }
         }
     }
@@ -372,29 +437,110 @@ __global__ __launch_bounds__(256) void join_kernel(const float *parts, int split
     }
 }
 
-template <int TM, int TN, int WM, int WN, bool EXACT, typename OUT>
-int run_tiles(const Product &p, OUT *C, void *workspace, size_t workspace_bytes, hipStream_t s)
+// How the kernel for few tokens splits a product; slices is 0 where the partial results do not fit the workspace.
+template <int MT, int NW>
+Stream plan_stream(const Product &p, size_t workspace_bytes)
 {
-    constexpr int BM = 16 * TM * WM, BN = 16 * TN * WN;
-    Tiling g;
-    g.n_tiles = ceil_div(p.N, BN);
-    g.tiles = g.n_tiles * ceil_div(p.M, BM);
-    if (g.tiles > kMaxTiles) return ZS_ERR_SHAPE;
+    Stream g;
+    g.n_tiles = ceil_div(p.N, 16);
     g.part_ld = (p.N + 3) / 4 * 4;
-    const int64_t cus = zs_compute_units();
-    int64_t splits = g.tiles >= cus ? 1 : cus / g.tiles;
-    splits = std::min(splits, p.k_blocks / 4); // at least four blocks each
-    splits = std::min(splits, workspace ? (int64_t)(workspace_bytes / (4 * (size_t)p.M * (size_t)g.part_ld)) : 0);
-    g.per_split = ceil_div(p.k_blocks, splits > 1 ? splits : 1);
-    g.splits = (int)ceil_div(p.k_blocks, g.per_split);
+    const int64_t fit = (int64_t)((kLds - stream_sums(MT, NW)) / stream_block((int)p.M)); // blocks of K that LDS holds
+    g.per_slice = ceil_div(p.k_blocks, ceil_div(p.k_blocks, fit));
+    g.slices = (int)ceil_div(p.k_blocks, g.per_slice);
+    if (g.slices > 1 && workspace_bytes / 4 / (size_t)g.slices / (size_t)p.M < (size_t)g.part_ld) g.slices = 0;
+    else g.wgs = (int)std::min(g.n_tiles, std::max((int64_t)1, zs_compute_units() / (int64_t)g.slices));
+    return g;
+}
+
+template <int MT, int NW, int D, bool W1, typename OUT>
+int run_stream(const Product &p, const Stream &g, OUT *C, void *workspace, hipStream_t s)
+{
+    const int rc = allow_lds<stream_kernel<MT, NW, D, W1, OUT>>(kLds);
+    if (rc != ZS_OK) return rc;
+    const dim3 grid((unsigned)(g.slices * g.wgs));
+    const size_t lds = stream_sums(MT, NW) + stream_block((int)p.M) * (size_t)g.per_slice;
+    float *parts = static_cast<float *>(workspace);
+    hipLaunchKernelGGL((stream_kernel<MT, NW, D, W1, OUT>), grid, dim3(64 * NW), lds, s, p, g, C, parts);
+    if (g.slices > 1)
+        hipLaunchKernelGGL(join_kernel<OUT>, dim3(grid_for(ceil_div(p.M * g.part_ld / 4, 256))), dim3(256), 0, s, parts, g.slices, g.part_ld, C,
+                           p.ldc, p.M, p.N);
+    return launched();
+}
+
+// Tile shapes, and what one of their blocks of 128 along K takes (us, measured with the GPU full of tiles of
+// 4096 x 8192 x 4096): `alone` with one workgroup to a compute unit, `two` for each of two that share one (0: LDS holds
+// one).  The numbers stand for FP32 results (FP16 instructions) and BF16 results (8-bit instructions).
+struct TileShape {
+    int tokens, features;
+    float alone[2], two[2];
+};
+constexpr TileShape kShapes[] = {{64, 128, {0.95f, 0.90f}, {1.20f, 0.85f}},
+                                 {128, 128, {1.45f, 1.05f}, {2.10f, 1.32f}},
+                                 {256, 128, {2.07f, 1.37f}, {0.f, 0.f}},
+                                 {256, 256, {0.f, 2.30f}, {0.f, 0.f}}};
+enum { kFp32 = 0, kBf16 = 1 };
+
+// The shape and number of splits along K with the least estimated time: rounds of workgroups times their blocks, and for splits
+// a second kernel (3 us, and the partial results there and back at 4 TB/s).
+struct TilePlan {
+    int shape;
+    Tiling g;
+};
+TilePlan plan_tiles(const Product &p, int kind, size_t workspace_bytes)
+{
+    const double cus = zs_compute_units();
+    const int64_t part_ld = (p.N + 3) / 4 * 4;
+    TilePlan best{-1, {}};
+    double least = 0;
+    for (int i = 0; i < (int)(sizeof kShapes / sizeof *kShapes); ++i) {
+        const TileShape &t = kShapes[i];
+        if (t.alone[kind] == 0.f) continue;
+        const int64_t n_tiles = ceil_div(p.N, t.features), tiles = n_tiles * ceil_div(p.M, t.tokens);
+        for (int64_t splits = 1; splits <= 16; ++splits) {
+            const int64_t per_split = ceil_div(p.k_blocks, splits);
+            if (splits > 1 && (ceil_div(p.k_blocks, per_split) != splits || per_split < 4 ||
+                               workspace_bytes / 4 / (size_t)splits / (size_t)p.M < (size_t)part_ld))
+                continue;
+            const double wgs = (double)tiles * (double)splits;
+            double time = std::ceil(wgs / cus) * t.alone[kind];
+            if (t.two[kind] != 0.f && wgs > cus) time = std::ceil(wgs / (2 * cus)) * t.two[kind];
+            time = time * (double)per_split + (splits > 1 ? 3.0 + (double)splits * (double)p.M * (double)part_ld * 8 / 4e6 : 0.0);
+            if (best.shape >= 0 && time >= least) continue;
+            least = time;
+            best = {i, {n_tiles, tiles, per_split, (int)splits, part_ld}};
+        }
+    }
+    return best;
+}
+
+template <int TM, int TN, int WM, int WN, int STAGES, typename OUT>
+int run_tiles(const Product &p, const Tiling &g, OUT *C, void *workspace, hipStream_t s)
+{
+    constexpr bool kExact = std::is_same_v<OUT, float>;
+    if (g.tiles * g.splits > kMaxTiles) return ZS_ERR_SHAPE;
     float *parts = static_cast<float *>(workspace);
     const dim3 grid((unsigned)(g.tiles * g.splits)), wg(64 * WM * WN);
-    if (p.w_rows == 1) hipLaunchKernelGGL((tiles_kernel<TM, TN, WM, WN, true, EXACT, OUT>), grid, wg, 0, s, p, g, C, parts);
-    else hipLaunchKernelGGL((tiles_kernel<TM, TN, WM, WN, false, EXACT, OUT>), grid, wg, 0, s, p, g, C, parts);
+    if (p.w_rows == 1) hipLaunchKernelGGL((tiles_kernel<TM, TN, WM, WN, STAGES, true, kExact, OUT>), grid, wg, 0, s, p, g, C, parts);
+    else hipLaunchKernelGGL((tiles_kernel<TM, TN, WM, WN, STAGES, false, kExact, OUT>), grid, wg, 0, s, p, g, C, parts);
     if (g.splits > 1)
         hipLaunchKernelGGL(join_kernel<OUT>, dim3(grid_for(ceil_div(p.M * g.part_ld / 4, 256))), dim3(256), 0, s, parts, g.splits, g.part_ld, C,
                            p.ldc, p.M, p.N);
     return launched();
+}
+
+template <typename OUT>
+int run_tiled(const Product &p, OUT *C, void *workspace, size_t workspace_bytes, hipStream_t s)
+{
+    constexpr bool kExact = std::is_same_v<OUT, float>;
+    const TilePlan plan = plan_tiles(p, kExact ? kFp32 : kBf16, workspace_bytes);
+    switch (plan.shape) {
+    case 0: return run_tiles<4, 2, 1, 4, kExact ? 2 : 3>(p, plan.g, C, workspace, s);
+    case 1: return run_tiles<2, 4, 4, 2, 2>(p, plan.g, C, workspace, s);
+    case 2: return run_tiles<4, 4, 4, 2, kExact ? 2 : 3>(p, plan.g, C, workspace, s);
+    default: break;
+    }
+    if constexpr (kExact) return ZS_ERR_HIP; // (no such plan)
+    else return run_tiles<4, 8, 4, 2, 2>(p, plan.g, C, workspace, s);
 }
 
 template <typename OUT>
@@ -409,14 +555,17 @@ int run(const uint8_t *A, int64_t lda, const float *SA, int64_t ldsa, const uint
     if (lda > kMaxLd || ldw > kMaxLd) return ZS_ERR_SHAPE; // offsets inside a tile are 32 bits wide
     const Product p = {A, W, SA, SW, lda, ldsa, ldw, ldsw, ldc, M, N, K, ceil_div(K, kBlock), w_rows};
     hipStream_t stream = static_cast<hipStream_t>(hip_stream);
-    if (M > 32) {
-        if (M <= 64) return run_tiles<4, 2, 1, 4, true>(p, C, workspace, workspace_bytes, stream);
-        constexpr bool kExact = std::is_same_v<OUT, float>;
-        if constexpr (kExact) return run_tiles<4, 4, 4, 2, true>(p, C, workspace, workspace_bytes, stream);
-        else return run_tiles<4, 8, 4, 2, false>(p, C, workspace, workspace_bytes, stream);
+    if (!workspace) workspace_bytes = 0;
+    if (M <= 16) {
+        const Stream g = plan_stream<1, 16>(p, workspace_bytes);
+        if (g.slices)
+            return w_rows == 1 ? run_stream<1, 16, 2, true>(p, g, C, workspace, stream) : run_stream<1, 16, 2, false>(p, g, C, workspace, stream);
+    } else if (M <= 32) {
+        const Stream g = plan_stream<2, 16>(p, workspace_bytes);
+        if (g.slices)
+            return w_rows == 1 ? run_stream<2, 16, 2, true>(p, g, C, workspace, stream) : run_stream<2, 16, 2, false>(p, g, C, workspace, stream);
     }
-    if (M > 16) return run_stream<2, 1, 8, 4>(p, C, stream);
-    return run_stream<1, 1, 8, 4>(p, C, stream);
+    return run_tiled(p, C, workspace, workspace_bytes, stream);
 }
 
 } // namespace

@@ -6,6 +6,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <atomic>
+
 #include "zipserv.h"
 
 namespace zs_ops {
@@ -74,6 +76,20 @@ __device__ __forceinline__ void load8(const float *p, int64_t left, float v[8])
 
 inline bool aligned(const void *p, uintptr_t to) { return reinterpret_cast<uintptr_t>(p) % to == 0; }
 inline int launched() { return hipGetLastError() == hipSuccess ? ZS_OK : ZS_ERR_HIP; }
+// Lets a kernel use up to `bytes` of dynamic LDS on the current device.  The attribute stays with (kernel, device):
+// `done` has a bit for each device that it was set on.
+template <auto Kernel>
+inline int allow_lds(size_t bytes)
+{
+    static std::atomic<uint64_t> done{0};
+    int device = 0;
+    if (hipGetDevice(&device) != hipSuccess || device < 0 || device >= 64) return ZS_ERR_HIP;
+    if (done.load(std::memory_order_acquire) >> device & 1u) return ZS_OK;
+    if (hipFuncSetAttribute(reinterpret_cast<const void *>(Kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes) != hipSuccess)
+        return ZS_ERR_HIP;
+    done.fetch_or(1ull << device, std::memory_order_release);
+    return ZS_OK;
+}
 // A launch counts its threads along x in 32 bits: kernels whose work could exceed that stride over it.
 inline unsigned grid_for(int64_t wgs, int64_t most = 1 << 20) { return (unsigned)(wgs < most ? wgs : most); }
 inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
