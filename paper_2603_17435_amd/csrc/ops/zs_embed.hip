@@ -1,6 +1,6 @@
 // Embedding operators: rows of a table by token ids, times a scale (zs_embed out of a compressed blob,
 // zs_dense_embed out of a BF16 matrix), and the gradient of the table (zs_embed_grad).
-#include "zs_format.h"
+#include "zs_device.h"
 #include "zs_ops.h"
 
 using namespace zs_ops;
@@ -29,20 +29,11 @@ struct Blob {
     int32_t k_blocks;
 };
 
-__device__ __forceinline__ uint32_t inclusive_scan(uint32_t x, int lane)
-{
-    for (int d = 1; d < 64; d *= 2) {
-        const uint32_t y = (uint32_t)__shfl_up((int)x, d);
-        x += lane >= d ? y : 0u;
-    }
-    return x;
-}
-
 __global__ __launch_bounds__(256) void embed_kernel(Blob b, int64_t N, const void *ids, int id_bytes, int64_t tasks, float scale,
                                                     uint16_t *Y, int64_t ldy)
 {
-    const int lane = threadIdx.x % 64;
-    for (int64_t task = (int64_t)blockIdx.x * 4 + threadIdx.x / 64; task < tasks; task += (int64_t)gridDim.x * 4) {
+    const uint32_t lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+    for (int64_t task = (int64_t)blockIdx.x * 4 + wave; task < tasks; task += (int64_t)gridDim.x * 4) {
         const int64_t t = task / b.k_blocks, kb = task - t * b.k_blocks;
         uint16_t *const out = Y + t * ldy + ZS_BT_DIM * kb + lane;
         const int64_t id = id_at(ids, id_bytes, t, N);
@@ -52,25 +43,34 @@ __global__ __launch_bounds__(256) void embed_kernel(Blob b, int64_t N, const voi
         }
         const int64_t bt = id / ZS_BT_DIM * b.k_blocks + kb;
         const uint32_t row = (uint32_t)(id % ZS_BT_DIM), r = row % 8;
-        const uint64_t *planes = reinterpret_cast<const uint64_t *>(b.bitmaps + bt * ZS_BT_BITMAP_BYTES) + 3 * lane;
-        const uint64_t p1 = planes[0], p2 = planes[1], p3 = planes[2], m = p1 | p2 | p3;
-        const uint64_t h_start = 16 * (uint64_t)b.offsets[2 * bt], l_start = 16 * (uint64_t)b.offsets[2 * bt + 1];
-        const uint32_t count = (uint32_t)__popcll(m);
-        const uint32_t start = inclusive_scan(count, lane) - count + (uint32_t)__popcll(m & ((1ull << (8 * r)) - 1));
-        const uint32_t bytes = (uint32_t)(p1 >> (8 * r) & 0xFF) | (uint32_t)(p2 >> (8 * r) & 0xFF) << 8 | (uint32_t)(p3 >> (8 * r) & 0xFF) << 16;
         // column `lane`: FragTile column lane / 8, which lies in TensorCoreTile column lane / 32
-        const uint32_t j = lane % 8, f = (lane / 32 * 4 + row / 16) * ZS_FT_PER_TT + lane / 8 % 4 * 2 + row / 8 % 2;
-        const uint32_t w = (uint32_t)__shfl((int)bytes, (int)f) >> j;
-        const uint32_t inside = (uint32_t)__shfl((int)(bytes | bytes >> 8 | bytes >> 16), (int)f) & 0xFFu;
-        const uint32_t hi = (uint32_t)__shfl((int)start, (int)f) + __popc(inside & ((1u << j) - 1u));
-        const uint32_t code = (w & 1u) | (w >> 8 & 1u) << 1 | (w >> 16 & 1u) << 2;
+        const uint32_t f_row = row / 16 * ZS_FT_PER_TT + row / 8 % 2, j = lane % 8;
+        const uint32_t f = lane / 32 * (4 * ZS_FT_PER_TT) + lane / 8 % 4 * 2 + f_row, f_last = 4 * ZS_FT_PER_TT + 6 + f_row;
+        u32x2 p1 = {0, 0}, p2 = {0, 0}, p3 = {0, 0};
+        if (lane <= f_last) { // (the FragTiles behind the row's last one do not matter)
+            const u32x2 *planes = reinterpret_cast<const u32x2 *>(b.bitmaps + bt * ZS_BT_BITMAP_BYTES) + 3 * lane;
+            p1 = planes[0];
+            p2 = planes[1];
+            p3 = planes[2];
+        }
+        const uint64_t h_start = 16 * (uint64_t)b.offsets[2 * bt], l_start = 16 * (uint64_t)b.offsets[2 * bt + 1];
+        const uint32_t lo = p1.x | p2.x | p3.x, hi = p1.y | p2.y | p3.y;
+        const uint64_t below = (1ull << (8 * r)) - 1; // of a FragTile, the rows above this one
+        const uint32_t count = __popc(lo) + __popc(hi);
+        const uint32_t start = zs::wave_inclusive_scan(count) - count + __popc(lo & (uint32_t)below) + __popc(hi & (uint32_t)(below >> 32));
+        const uint32_t at = 8 * (r % 4);
+        auto byte = [&](u32x2 p) { return (r < 4 ? p.x : p.y) >> at & 0xFFu; };
+        const uint32_t bytes = byte(p1) | byte(p2) << 8 | byte(p3) << 16;
+        const uint32_t w = (uint32_t)__shfl((int)bytes, (int)f), m = (w | w >> 8 | w >> 16) & 0xFFu;
+        const uint32_t h_at = (uint32_t)__shfl((int)start, (int)f) + __popc(m & ((1u << j) - 1u));
+        const uint32_t code = (w >> j & 1u) | (w >> (j + 8) & 1u) << 1 | (w >> (j + 16) & 1u) << 2;
         uint32_t value;
         if (code) {
-            const uint32_t h = b.H[min(h_start + hi, b.h_last)];
+            const uint32_t h = b.H[min(h_start + h_at, b.h_last)];
             value = (h & 0x80u) << 8 | ((uint32_t)(b.base_exp + (int)code) & 0xFFu) << 7 | (h & 0x7Fu);
         } else {
-            const uint32_t li = 64 * f + 8 * r + j - hi;
-            value = *reinterpret_cast<const uint16_t *>(b.L + min(l_start + 2 * li, b.l_last));
+            const uint32_t l_at = 64 * f + 8 * r + j - h_at;
+            value = *reinterpret_cast<const uint16_t *>(b.L + min(l_start + 2 * l_at, b.l_last));
         }
         *out = bf16_bits(bf16_value(value) * scale);
     }
@@ -124,10 +124,32 @@ constexpr uint32_t kNoRow = 0xFFFFFFFFu;
 
 typedef uint64_t Pair; // id << 32 | position: all different, so that a pair's place is a count of smaller ones
 
-__global__ __launch_bounds__(kTile) void sort_tiles_kernel(const void *ids, int id_bytes, int64_t T, int64_t N, Pair *out)
+// Zeros for `rows` rows of `cols` elements (a dW without gaps is one row), by `wgs` workgroups of which this is `wg`.
+struct Zeros {
+    float *p;
+    int64_t rows, cols, ld;
+};
+__device__ __forceinline__ void clear(const Zeros &z, int64_t wg, int64_t wgs)
+{
+    const int64_t across = z.rows == 1 ? wgs : 1; // workgroups that share a row
+    for (int64_t r = z.rows == 1 ? 0 : wg; r < z.rows; r += wgs)
+        for (int64_t c = 4 * ((z.rows == 1 ? wg * blockDim.x : 0) + threadIdx.x); c < z.cols; c += 4 * across * blockDim.x) {
+            float *q = z.p + r * z.ld + c;
+            if (c + 4 <= z.cols) store_any(q, f32x4{0.f, 0.f, 0.f, 0.f});
+            else
+                for (int64_t i = 0; i < z.cols - c; ++i) q[i] = 0.f;
+        }
+}
+
+// Sorts kTile pairs in each of the first `tiles` workgroups; the others clear their part of dW meanwhile.
+__global__ __launch_bounds__(kTile) void sort_tiles_kernel(const void *ids, int id_bytes, int64_t T, int64_t N, Pair *out, int tiles, Zeros z)
 {
     __shared__ Pair keys[kTile];
     const int tid = threadIdx.x;
+    if ((int)blockIdx.x >= tiles) {
+        clear(z, blockIdx.x - tiles, gridDim.x - tiles);
+        return;
+    }
     const int64_t t = (int64_t)blockIdx.x * kTile + tid;
     Pair mine = ~0ull;
     if (t < T) {
@@ -152,37 +174,33 @@ __global__ __launch_bounds__(kTile) void sort_tiles_kernel(const void *ids, int 
     if (t < T) out[t] = mine;
 }
 
-// Sorted lists of `run` pairs become lists of run * kFan: a pair's place is its own index plus the number of smaller
-// pairs in each of the other lists of its group.
-__global__ __launch_bounds__(256) void merge_kernel(const Pair *in, Pair *out, int64_t T, int64_t run)
+// Sorted lists of `run` pairs (a power of two) become lists of run * kFan: a pair's place is its own index plus the
+// number of smaller pairs in each of the other lists of its group, searched for in all of them at a time.
+__device__ __forceinline__ void merge(const Pair *in, Pair *out, int64_t T, int64_t run, int64_t t)
 {
-    for (int64_t t = (int64_t)blockIdx.x * 256 + threadIdx.x; t < T; t += (int64_t)gridDim.x * 256) {
-        const Pair mine = in[t];
-        const int64_t group = t / (run * kFan) * (run * kFan), own = t / run * run;
-        int64_t place = group + (t - own);
-        for (int64_t l = group; l < min(group + run * kFan, T); l += run) {
-            if (l == own) continue;
-            int64_t lo = 0, hi = min(run, T - l); // smaller pairs of this list: at least lo, at most hi
-            while (lo < hi) {
-                const int64_t mid = (lo + hi) / 2;
-                if (in[l + mid] < mine) lo = mid + 1;
-                else hi = mid;
-            }
-            place += lo;
+    const Pair mine = in[t];
+    const int64_t group = t / (run * kFan) * (run * kFan);
+    int64_t smaller[kFan] = {};
+    for (int64_t step = run; step > 0; step /= 2)
+#pragma unroll
+        for (int l = 0; l < kFan; ++l) {
+            const int64_t list = group + l * run, to = list + smaller[l] + step;
+            if (smaller[l] + step <= run && to <= T && in[to - 1] < mine) smaller[l] += step;
         }
-        out[place] = mine;
-    }
+    int64_t place = group;
+#pragma unroll
+    for (int l = 0; l < kFan; ++l) place += smaller[l];
+    out[place] = mine;
 }
 
-__global__ __launch_bounds__(256) void zero_rows_kernel(float *dW, int64_t K, int64_t ldw, int64_t units, int64_t row_units)
+// Merges in the first `wgs` workgroups; the others clear their part of dW meanwhile.
+__global__ __launch_bounds__(256) void merge_kernel(const Pair *in, Pair *out, int64_t T, int64_t run, int wgs, Zeros z)
 {
-    for (int64_t u = (int64_t)blockIdx.x * 256 + threadIdx.x; u < units; u += (int64_t)gridDim.x * 256) {
-        const int64_t r = u / row_units, c = 4 * (u - r * row_units);
-        float *p = dW + r * ldw + c;
-        if (c + 4 <= K) store_any(p, f32x4{0.f, 0.f, 0.f, 0.f});
-        else
-            for (int64_t i = c; i < K; ++i) dW[r * ldw + i] = 0.f;
+    if ((int)blockIdx.x >= wgs) {
+        clear(z, blockIdx.x - wgs, gridDim.x - wgs);
+        return;
     }
+    for (int64_t t = (int64_t)blockIdx.x * 256 + threadIdx.x; t < T; t += (int64_t)wgs * 256) merge(in, out, T, run, t);
 }
 
 struct Runs {
@@ -217,62 +235,89 @@ __device__ __forceinline__ void put(float *p, const float v[kCols], int64_t left
 template <typename T>
 __global__ __launch_bounds__(64) void sum_kernel(Runs g, const T *dY, int64_t lddy, float scale, float *dW, int64_t ldw, int add)
 {
+    constexpr int kAhead = sizeof(T) == 2 ? 16 : 8; // rows of dY requested at a time
     for (int64_t task = blockIdx.x; task < g.chunks * g.slices; task += gridDim.x) {
         const int64_t chunk = task / g.slices, c = ((task - chunk * g.slices) * 64 + threadIdx.x) * kCols, left = g.K - c;
-        const int64_t begin = chunk * g.chunk, end = min(begin + g.chunk, g.T);
-        if (left <= 0) continue;
-        const uint32_t before = g.id_before(begin), behind = g.id_behind(end);
+        const int64_t begin = chunk * g.chunk;
+        const int size = (int)min((int64_t)g.chunk, g.T - begin);
+        // the chunk's pairs, one to a lane, and the ids on both sides; tokens without a row are the last ones
+        const Pair mine = g.pairs[begin + min((int)threadIdx.x, size - 1)];
+        const uint32_t before = g.id_before(begin), behind = g.id_behind(begin + size);
+        const int n = __builtin_popcountll(__builtin_amdgcn_ballot_w64((int)threadIdx.x < size && (uint32_t)(mine >> 32) != kNoRow));
         float acc[kCols] = {};
-        for (int64_t i = begin; i < end; ++i) {
-            const Pair pair = g.pairs[i];
-            const uint32_t id = (uint32_t)(pair >> 32);
-            if (id == kNoRow) break; // only tokens without a row follow
-            float v[kCols];
-            load8(dY + (int64_t)(uint32_t)pair * lddy + c, left, v);
+        for (int i0 = 0; i0 < n; i0 += kAhead) {
+            Eight<T> v[kAhead];
 #pragma unroll
-            for (int j = 0; j < kCols; ++j) acc[j] += v[j];
-            const uint32_t next = i + 1 < end ? g.id(i + 1) : behind;
-            if (i + 1 < end && next == id) continue;
-            // the run's sum over this chunk
-            if (id == before) put(g.heads + chunk * g.K + c, acc, left, 1.f, false);
-            else if (id == next) put(g.tails + chunk * g.K + c, acc, left, 1.f, false);
-            else put(dW + (int64_t)id * ldw + c, acc, left, scale, add);
+            for (int i = 0; i < kAhead; ++i) {
+                const int64_t t = (int64_t)(uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)mine, min(i0 + i, n - 1));
+                v[i] = fetch8(dY + t * lddy + c, left);
+            }
 #pragma unroll
-            for (int j = 0; j < kCols; ++j) acc[j] = 0.f;
+            for (int i = 0; i < kAhead; ++i) {
+                const int at = i0 + i;
+                if (at >= n) break;
+                const uint32_t id = (uint32_t)__builtin_amdgcn_readlane((int)(mine >> 32), at);
+#pragma unroll
+                for (int j = 0; j < kCols; ++j) acc[j] += value8(v[i], j);
+                const uint32_t next = at + 1 < n ? (uint32_t)__builtin_amdgcn_readlane((int)(mine >> 32), at + 1) : behind;
+                if (at + 1 < n && next == id) continue;
+                // the run's sum over this chunk
+                if (id == before) put(g.heads + chunk * g.K + c, acc, left, 1.f, false);
+                else if (id == next) put(g.tails + chunk * g.K + c, acc, left, 1.f, false);
+                else put(dW + (int64_t)id * ldw + c, acc, left, scale, add);
+#pragma unroll
+                for (int j = 0; j < kCols; ++j) acc[j] = 0.f;
+            }
         }
     }
 }
 
-// Runs over several chunks: the chunk in which one begins adds up what the chunks behind it left.
+// Runs over several chunks: the chunk in which one begins adds up what the chunks behind it left, in their order.
 __global__ __launch_bounds__(64) void join_kernel(Runs g, float scale, float *dW, int64_t ldw, int add)
 {
+    constexpr int kAhead = 8;
     for (int64_t task = blockIdx.x; task < (g.chunks - 1) * g.slices; task += gridDim.x) {
         const int64_t chunk = task / g.slices, c = ((task - chunk * g.slices) * 64 + threadIdx.x) * kCols, left = g.K - c;
         const int64_t begin = chunk * g.chunk, end = begin + g.chunk;
         const uint32_t id = g.id(end - 1);
-        if (left <= 0 || id == kNoRow || id != g.id(end) || id == g.id_before(begin)) continue;
-        float acc[kCols], v[kCols];
+        if (id == kNoRow || id != g.id(end) || id == g.id_before(begin)) continue;
+        float acc[kCols];
         load8(g.tails + chunk * g.K + c, left, acc);
-        for (int64_t k = chunk + 1; k < g.chunks && g.id(k * g.chunk) == id; ++k) {
-            load8(g.heads + k * g.K + c, left, v);
+        for (int64_t k = chunk + 1; k < g.chunks;) {
+            // of the next 64 chunks, those that begin inside the run: the first ones
+            const int64_t mine = k + threadIdx.x;
+            const uint64_t inside = __builtin_amdgcn_ballot_w64(mine < g.chunks && g.id(min(mine, g.chunks - 1) * g.chunk) == id);
+            const int n = inside == ~0ull ? 64 : __builtin_ctzll(~inside);
+            for (int i0 = 0; i0 < n; i0 += kAhead) {
+                float v[kAhead][kCols];
 #pragma unroll
-            for (int j = 0; j < kCols; ++j) acc[j] += v[j];
+                for (int i = 0; i < kAhead; ++i) load8(g.heads + (k + min(i0 + i, n - 1)) * g.K + c, left, v[i]);
+#pragma unroll
+                for (int i = 0; i < kAhead; ++i)
+                    if (i0 + i < n)
+#pragma unroll
+                        for (int j = 0; j < kCols; ++j) acc[j] += v[i][j];
+            }
+            if (n < 64) break;
+            k += 64;
         }
         put(dW + (int64_t)id * ldw + c, acc, left, scale, add);
     }
 }
 
-constexpr int kChunk = 32;
-
 struct GradPlan {
-    int64_t chunks;
+    int chunk; // tokens
+    int64_t chunks, slices;
     size_t pairs_bytes, sums_bytes, total;
 };
 GradPlan plan_grad(int64_t T, int64_t K)
 {
     GradPlan p;
     auto up = [](size_t x) { return (x + 255) / 256 * 256; };
-    p.chunks = ceil_div(T, kChunk);
+    // 32 tokens to a chunk where that makes 1024 waves or more, else 8: more waves, more partial sums
+    p.slices = ceil_div(K, 64 * kCols);
+    p.chunk = ceil_div(T, 32) * p.slices >= 1024 ? 32 : 8;
+    p.chunks = ceil_div(T, p.chunk);
     p.pairs_bytes = up(8 * (size_t)T);
     p.sums_bytes = up(4 * (size_t)p.chunks * (size_t)K);
     p.total = 2 * p.pairs_bytes + 2 * p.sums_bytes;
@@ -342,27 +387,42 @@ extern "C" int zs_embed_grad(const void *ids_dev, int id_bytes, int64_t T, const
     const GradPlan plan = plan_grad(T, K);
     if (workspace_bytes < plan.total) return ZS_ERR_SIZE;
     hipStream_t s = static_cast<hipStream_t>(hip_stream);
-    if (!accumulate) {
-        const int64_t row_units = ceil_div(K, 4), units = N * row_units;
-        hipLaunchKernelGGL(zero_rows_kernel, dim3(grid_for(ceil_div(units, 256))), dim3(256), 0, s, dW_dev, K, lddw, units, row_units);
+    // dW is cleared by workgroups beside the ones that sort, half of it beside a merge if there is one
+    const bool whole = lddw == K;
+    const int64_t rows = accumulate ? 0 : whole ? 1 : N, cols = whole ? N * K : K;
+    Zeros first = {dW_dev, rows, cols, lddw}, second = {dW_dev, 0, cols, lddw};
+    if (T > kTile && rows == 1) {
+        first.cols = cols / 8 * 4;
+        second = {dW_dev + first.cols, 1, cols - first.cols, lddw};
+    } else if (T > kTile) {
+        first.rows = rows / 2;
+        second = {dW_dev + first.rows * lddw, rows - first.rows, cols, lddw};
     }
-    if (T == 0) return launched();
+    const Zeros none = {nullptr, 0, 0, 0};
+    const int tiles = (int)ceil_div(T, kTile);
+    auto clearing = [](const Zeros &z, int threads) {
+        return (unsigned)(z.rows == 0 ? 0 : grid_for(z.rows == 1 ? ceil_div(z.cols, 4 * threads) : z.rows, (1 << 28) / threads));
+    };
     uint8_t *ws = static_cast<uint8_t *>(workspace_dev);
     Pair *from = reinterpret_cast<Pair *>(ws), *to = reinterpret_cast<Pair *>(ws + plan.pairs_bytes);
-    hipLaunchKernelGGL(sort_tiles_kernel, dim3((unsigned)ceil_div(T, kTile)), dim3(kTile), 0, s, ids_dev, id_bytes, T, N, from);
+    if (tiles + clearing(first, kTile))
+        hipLaunchKernelGGL(sort_tiles_kernel, dim3(tiles + clearing(first, kTile)), dim3(kTile), 0, s, ids_dev, id_bytes, T, N, from, tiles, first);
     for (int64_t run = kTile; run < T; run *= kFan) {
-        hipLaunchKernelGGL(merge_kernel, dim3(grid_for(ceil_div(T, 256))), dim3(256), 0, s, from, to, T, run);
+        const Zeros &z = run == kTile ? second : none;
+        const int wgs = (int)grid_for(ceil_div(T, 256));
+        hipLaunchKernelGGL(merge_kernel, dim3(wgs + clearing(z, 256)), dim3(256), 0, s, from, to, T, run, wgs, z);
         Pair *const swap = from;
         from = to;
         to = swap;
     }
+    if (T == 0) return launched();
     Runs g;
     g.pairs = from;
     g.T = T;
     g.K = K;
-    g.slices = ceil_div(K, 64 * kCols);
+    g.slices = plan.slices;
     g.chunks = plan.chunks;
-    g.chunk = kChunk;
+    g.chunk = plan.chunk;
     g.heads = reinterpret_cast<float *>(ws + 2 * plan.pairs_bytes);
     g.tails = reinterpret_cast<float *>(ws + 2 * plan.pairs_bytes + plan.sums_bytes);
     const dim3 grid(grid_for(g.chunks * g.slices));

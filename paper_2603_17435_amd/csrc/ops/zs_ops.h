@@ -44,34 +44,36 @@ __device__ __forceinline__ uint32_t bf16_pair(float lo, float hi)
     return __builtin_bit_cast(uint32_t, bf16x2{(__bf16)lo, (__bf16)hi});
 }
 
-// Eight consecutive values of a row of BF16 patterns or floats; those at and behind `left` are zero.
-__device__ __forceinline__ void load8(const uint16_t *p, int64_t left, float v[8])
+// Eight consecutive values of a row of BF16 patterns or floats as they lie there; those at and behind `left` are zero.
+template <typename T>
+struct Eight {
+    u32x4 w[sizeof(T) / 2];
+};
+template <typename T>
+__device__ __forceinline__ Eight<T> fetch8(const T *p, int64_t left)
 {
-    if (left >= 8) {
-        const u32x4 w = load_any<u32x4>(p);
+    if (left >= 8) return load_any<Eight<T>>(p);
+    Eight<T> e = {};
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            v[2 * i] = bf16_value(w[i] & 0xFFFFu);
-            v[2 * i + 1] = __builtin_bit_cast(float, w[i] & 0xFFFF0000u);
+    for (int i = 0; i < 8; ++i)
+        if (i < left) {
+            if constexpr (sizeof(T) == 2) e.w[0][i / 2] |= (uint32_t)p[i] << (16 * (i % 2));
+            else e.w[i / 4][i % 4] = __builtin_bit_cast(uint32_t, p[i]);
         }
-        return;
-    }
-#pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = i < left ? bf16_value(p[i]) : 0.f;
+    return e;
 }
-__device__ __forceinline__ void load8(const float *p, int64_t left, float v[8])
+template <typename T>
+__device__ __forceinline__ float value8(const Eight<T> &e, int i) // i is a constant
 {
-    if (left >= 8) {
-        const f32x4 a = load_any<f32x4>(p), b = load_any<f32x4>(p + 4);
+    const uint32_t w = sizeof(T) == 2 ? e.w[0][i / 2] : e.w[(i / 4) % (sizeof(T) / 2)][i % 4];
+    return __builtin_bit_cast(float, sizeof(T) == 4 ? w : i % 2 ? w & 0xFFFF0000u : w << 16);
+}
+template <typename T>
+__device__ __forceinline__ void load8(const T *p, int64_t left, float v[8])
+{
+    const Eight<T> e = fetch8(p, left);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            v[i] = a[i];
-            v[4 + i] = b[i];
-        }
-        return;
-    }
-#pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = i < left ? p[i] : 0.f;
+    for (int i = 0; i < 8; ++i) v[i] = value8(e, i);
 }
 
 inline bool aligned(const void *p, uintptr_t to) { return reinterpret_cast<uintptr_t>(p) % to == 0; }
