@@ -141,6 +141,20 @@ __device__ __forceinline__ void clear(const Zeros &z, int64_t wg, int64_t wgs)
         }
 }
 
+// The value of the lane whose number differs in bit d (a constant): within a row of sixteen lanes by moves of the
+// vector unit where it has one, else through the LDS crossbar.
+__device__ __forceinline__ uint32_t partner(uint32_t x, int d)
+{
+    switch (d) {
+    case 1: return __builtin_amdgcn_update_dpp(0u, x, 0xB1, 0xf, 0xf, false);  // quad_perm 1, 0, 3, 2
+    case 2: return __builtin_amdgcn_update_dpp(0u, x, 0x4E, 0xf, 0xf, false);  // quad_perm 2, 3, 0, 1
+    case 4: return (uint32_t)__builtin_amdgcn_ds_swizzle((int)x, 0x101F);      // xor 4
+    case 8: return __builtin_amdgcn_update_dpp(0u, x, 0x128, 0xf, 0xf, false); // row_ror:8
+    case 16: return (uint32_t)__builtin_amdgcn_ds_swizzle((int)x, 0x401F);     // xor 16
+    default: return (uint32_t)__shfl_xor((int)x, 32);
+    }
+}
+
 // Sorts kTile pairs in each of the first `tiles` workgroups; the others clear their part of dW meanwhile.
 __global__ __launch_bounds__(kTile) void sort_tiles_kernel(const void *ids, int id_bytes, int64_t T, int64_t N, Pair *out, int tiles, Zeros z)
 {
@@ -156,12 +170,14 @@ __global__ __launch_bounds__(kTile) void sort_tiles_kernel(const void *ids, int 
         const int64_t id = id_at(ids, id_bytes, t, N);
         mine = (Pair)(id < 0 ? kNoRow : (uint32_t)id) << 32 | (uint32_t)t;
     }
-    // bitonic sorting network: partners less than a wave apart meet in registers
+    // bitonic sorting network: partners less than a wave apart meet in registers, the others in LDS
+#pragma unroll
     for (int size = 2; size <= kTile; size *= 2)
+#pragma unroll
         for (int d = size / 2; d > 0; d /= 2) {
             Pair other;
             if (d < 64) {
-                other = (Pair)__shfl_xor((unsigned long long)mine, d);
+                other = (Pair)partner((uint32_t)(mine >> 32), d) << 32 | partner((uint32_t)mine, d);
             } else {
                 keys[tid] = mine;
                 __syncthreads();
