@@ -244,6 +244,49 @@ struct Tiling {
     int64_t part_ld;        // row length of the partial results (splits > 1)
 };
 
+// A wave's 16 TM x 16 TN results to memory.  A lane holds four features of one token, so that direct stores would leave
+// in pieces of 32 or 64 bytes of sixteen rows; through LDS, sixteen tokens at a time, they leave as whole rows of the tile.
+// 4096 x 8192 x 128: FP32 results 57 -> 36 us, BF16 28 -> 19.  `room`: LDS of this wave alone.
+template <int TM, int TN, typename T>
+__device__ __forceinline__ void store_tile(T *to, int64_t ld, const f32x4 (&acc)[TM][TN], uint32_t room, int lane, int64_t rows, int64_t cols)
+{
+    constexpr int kRow = 16 * TN * (int)sizeof(T), kChunks = kRow / 16, kPerChunk = 16 / (int)sizeof(T); // a chunk c lies at c ^ (row % kChunks)
+    const int row = lane % 16, part = lane / 16;
+#pragma unroll
+    for (int i = 0; i < TM; ++i) {
+#pragma unroll
+        for (int j = 0; j < TN; ++j) {
+            if constexpr (sizeof(T) == 4) {
+                *(__attribute__((address_space(3))) f32x4 *)(room + row * kRow + 16 * ((4 * j + part) ^ (row % kChunks))) = acc[i][j];
+            } else {
+                const f32x4 v = acc[i][j];
+                *(__attribute__((address_space(3))) u32x2 *)(room + row * kRow + 16 * ((2 * j + part / 2) ^ (row % kChunks)) + 8 * (part % 2)) =
+                    u32x2{bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3])};
+            }
+        }
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+#pragma unroll
+        for (int k = 0; k < kChunks / 4; ++k) {
+            const int r = (64 * k + lane) / kChunks, c = (64 * k + lane) % kChunks;
+            const u32x4 v = *(LdsU32x4)(room + r * kRow + 16 * (c ^ (r % kChunks)));
+            const int64_t left = cols - kPerChunk * c;
+            T *const q = to + (16 * i + r) * ld + kPerChunk * c;
+            if (16 * i + r >= rows || left <= 0) continue;
+            if (left >= kPerChunk) {
+                store_any(q, v);
+            } else {
+#pragma unroll
+                for (int e = 0; e < kPerChunk; ++e)
+                    if (e < left) {
+                        if constexpr (sizeof(T) == 4) q[e] = __builtin_bit_cast(f32x4, v)[e];
+                        else q[e] = (uint16_t)(v[e / 2] >> (16 * (e % 2)));
+                    }
+            }
+        }
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); // (read before the next sixteen tokens are written)
+    }
+}
+
 // The tile that a workgroup computes.  Workgroups go round over the eight XCDs, each with an L2 of its own: an XCD
 // takes a contiguous range of the tiles, which lie in bands of eight along the tokens, so that the range shares rows
 // of both operands.
@@ -410,17 +453,11 @@ __global__ __launch_bounds__(64 * WM * WN) void tiles_kernel(Product p, Tiling g
         }
     }
 
-#pragma unroll
-    for (int i = 0; i < TM; ++i) {
-        const int64_t m = m0 + 16 * (TM * wm + i) + row;
-#pragma unroll
-        for (int j = 0; j < TN; ++j) {
-            const int64_t n = n0 + 16 * (TN * wn + j) + 4 * part;
-            if (m >= p.M || n >= p.N) continue;
-            if (g.splits > 1) store4(parts + ((int64_t)split * p.M + m) * g.part_ld + n, acc[i][j], p.N - n);
-            else store4(C + m * p.ldc + n, acc[i][j], p.N - n);
-        }
-    }
+    barrier(); // LDS holds results from here on
+    const int64_t m = m0 + 16 * TM * wm, n = n0 + 16 * TN * wn;
+    const uint32_t room = lds + wave * (kStage * STAGES / kWaves / 1024 * 1024);
+    if (g.splits > 1) store_tile<TM, TN>(parts + ((int64_t)split * p.M + m) * g.part_ld + n, g.part_ld, acc, room, lane, p.M - m, p.N - n);
+    else store_tile<TM, TN>(C + m * p.ldc + n, p.ldc, acc, room, lane, p.M - m, p.N - n);
 }
 
 // The partial results of the splits, added in their order.
@@ -467,21 +504,27 @@ int run_stream(const Product &p, const Stream &g, OUT *C, void *workspace, hipSt
     return launched();
 }
 
-// Tile shapes, and what one of their blocks of 128 along K takes (us, measured with the GPU full of tiles of
-// 4096 x 8192 x 4096): `alone` with one workgroup to a compute unit, `two` for each of two that share one (0: LDS holds
-// one).  The numbers stand for FP32 results (FP16 instructions) and BF16 results (8-bit instructions).
+// Tile shapes and what a round of them takes (us), with one workgroup to a compute unit (`alone`) or two: `start` for its
+// first loads and its results, `block` for each block of 128 along K (0: LDS holds one).  For FP32 results (FP16
+// instructions) and BF16 results (8-bit instructions).  From 4096 x 14336 with 200, 512 and 1024 tokens, 256 tiles with K of
+// 1024 and 8192, and 4096 x 8192 with K of 128, 1024 and 4096.
+struct RoundTime {
+    float start, block;
+};
 struct TileShape {
     int tokens, features;
-    float alone[2], two[2];
+    RoundTime alone[2], two[2];
 };
-constexpr TileShape kShapes[] = {{64, 128, {0.95f, 0.90f}, {1.20f, 0.85f}},
-                                 {128, 128, {1.45f, 1.05f}, {2.10f, 1.32f}},
-                                 {256, 128, {2.07f, 1.37f}, {0.f, 0.f}},
-                                 {256, 256, {0.f, 2.30f}, {0.f, 0.f}}};
+constexpr TileShape kShapes[] = {{64, 128, {{1.5f, 0.81f}, {1.0f, 0.53f}}, {{2.7f, 1.08f}, {3.3f, 0.71f}}},
+                                 {128, 128, {{3.4f, 1.05f}, {1.4f, 0.88f}}, {{4.5f, 1.95f}, {4.9f, 1.08f}}},
+                                 {128, 128, {{}, {1.5f, 0.71f}}, {}}, // four blocks in LDS instead of two: fits once
+                                 {256, 128, {{6.0f, 1.80f}, {3.6f, 1.14f}}, {}},
+                                 {256, 256, {{}, {6.0f, 1.80f}}, {}}};
 enum { kFp32 = 0, kBf16 = 1 };
 
-// The shape and number of splits along K with the least estimated time: rounds of workgroups times their blocks, and for splits
-// a second kernel (3 us, and the partial results there and back at 4 TB/s).
+// The shape and number of splits along K with the least estimated time: rounds of workgroups times their blocks, no less than
+// the operands' way from memory, and for splits a second kernel (3 us, and the partial results there and back at 6.5 TB/s:
+// they stay in the last cache).
 struct TilePlan {
     int shape;
     Tiling g;
@@ -490,11 +533,12 @@ TilePlan plan_tiles(const Product &p, int kind, size_t workspace_bytes)
 {
     const double cus = zs_compute_units();
     const int64_t part_ld = (p.N + 3) / 4 * 4;
+    const double traffic = ((double)p.N + (double)p.M) * (double)p.K / 4.5e6; // the operands once, at 4.5 TB/s
     TilePlan best{-1, {}};
     double least = 0;
     for (int i = 0; i < (int)(sizeof kShapes / sizeof *kShapes); ++i) {
         const TileShape &t = kShapes[i];
-        if (t.alone[kind] == 0.f) continue;
+        if (t.alone[kind].block == 0.f) continue;
         const int64_t n_tiles = ceil_div(p.N, t.features), tiles = n_tiles * ceil_div(p.M, t.tokens);
         for (int64_t splits = 1; splits <= 16; ++splits) {
             const int64_t per_split = ceil_div(p.k_blocks, splits);
@@ -502,9 +546,11 @@ TilePlan plan_tiles(const Product &p, int kind, size_t workspace_bytes)
                                workspace_bytes / 4 / (size_t)splits / (size_t)p.M < (size_t)part_ld))
                 continue;
             const double wgs = (double)tiles * (double)splits;
-            double time = std::ceil(wgs / cus) * t.alone[kind];
-            if (t.two[kind] != 0.f && wgs > cus) time = std::ceil(wgs / (2 * cus)) * t.two[kind];
-            time = time * (double)per_split + (splits > 1 ? 3.0 + (double)splits * (double)p.M * (double)part_ld * 8 / 4e6 : 0.0);
+            const bool pairs = t.two[kind].block != 0.f && wgs > cus;
+            const RoundTime &round = pairs ? t.two[kind] : t.alone[kind];
+            double time = std::ceil(wgs / (pairs ? 2 * cus : cus)) * (round.start + (double)per_split * round.block);
+            time = std::max(time, traffic) + 0.1 * time; // (of those that wait for memory, the one with less to do)
+            if (splits > 1) time += 3.0 + (double)splits * (double)p.M * (double)part_ld * 8 / 6.5e6;
             if (best.shape >= 0 && time >= least) continue;
             least = time;
             best = {i, {n_tiles, tiles, per_split, (int)splits, part_ld}};
@@ -536,11 +582,11 @@ int run_tiled(const Product &p, OUT *C, void *workspace, size_t workspace_bytes,
     switch (plan.shape) {
     case 0: return run_tiles<4, 2, 1, 4, kExact ? 2 : 3>(p, plan.g, C, workspace, s);
     case 1: return run_tiles<2, 4, 4, 2, 2>(p, plan.g, C, workspace, s);
-    case 2: return run_tiles<4, 4, 4, 2, kExact ? 2 : 3>(p, plan.g, C, workspace, s);
+    case 3: return run_tiles<4, 4, 4, 2, kExact ? 2 : 3>(p, plan.g, C, workspace, s);
     default: break;
     }
     if constexpr (kExact) return ZS_ERR_HIP; // (no such plan)
-    else return run_tiles<4, 8, 4, 2, 2>(p, plan.g, C, workspace, s);
+    else return plan.shape == 2 ? run_tiles<2, 4, 4, 2, 4>(p, plan.g, C, workspace, s) : run_tiles<4, 8, 4, 2, 2>(p, plan.g, C, workspace, s);
 }
 
 template <typename OUT>
