@@ -131,7 +131,8 @@ def _ptr(x) -> ctypes.c_void_p:
 def _stream(stream) -> ctypes.c_void_p:
     if stream is None:
         import torch
-        stream = torch.cuda.current_stream()
+        raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)  # (the Stream object costs 2.6 us, a call of ours 4.5)
+        stream = raw(torch.cuda.current_device()) if raw else torch.cuda.current_stream()
     return ctypes.c_void_p(getattr(stream, "cuda_stream", stream))
 
 

@@ -59,33 +59,27 @@ __device__ __forceinline__ void store4(uint16_t *p, f32x4 v, int64_t left)
 }
 
 // ---- few tokens: the weights are read once ----------------------------------------------------
-// A workgroup keeps all M <= 16 MT tokens' codes of a slice of K in LDS and multiplies them by one tile of 16 features after
+// A workgroup keeps the codes of all M <= 16 tokens in LDS and multiplies them by one tile of 16 features after
 // another.  Its NW waves share a tile's blocks of 128 along K and add their sums up in LDS, always in the same order.
 // Each wave requests its blocks of W, of this tile and the next ones, D ahead, straight into operand registers: a lane
 // takes the chunks of 16 bytes `part` and `part` + 4 of its row, so that a load covers 64 contiguous bytes
-// of sixteen rows.  W is the first operand, so a lane holds four features of one token.
+// of sixteen rows.  W is the first operand, so a lane holds four features of one token.  Bound by the weights' way from
+// memory: 28672 x 4096 takes 25 us for one token (4.7 TB/s) and 29 us for sixteen, whose codes in LDS save 6 us
+// over fetching them from the L2 for every tile.
 constexpr size_t kLds = 160 * 1024;
-constexpr size_t stream_sums(int mt, int waves) { return (size_t)2 * waves * mt * 1024; }
+constexpr size_t stream_sums(int waves) { return (size_t)2 * waves * 1024; }
 constexpr size_t stream_block(int rows) { return (size_t)rows * (kBlock + 4); } // a block's codes and scales
 
-struct Stream {
-    int64_t n_tiles;
-    int64_t per_slice; // blocks of K in a slice
-    int slices, wgs;   // workgroups of a slice
-    int64_t part_ld;   // row length of the partial results (slices > 1)
-};
-
-template <int MT, int NW, int D, bool W1, typename OUT>
-__global__ __launch_bounds__(64 * NW) void stream_kernel(Product p, Stream g, OUT *C, float *parts)
+template <int NW, int D, bool W1, typename OUT>
+__global__ __launch_bounds__(64 * NW) void stream_kernel(Product p, OUT *C)
 {
     extern __shared__ __attribute__((aligned(16))) uint8_t smem[];
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), row = lane % 16, part = lane / 16;
-    const int slice = blockIdx.x / g.wgs, first = blockIdx.x - slice * g.wgs;
-    const int64_t kb0 = slice * g.per_slice;
-    const int blocks = (int)min(g.per_slice, p.k_blocks - kb0), rows = (int)p.M;
-    const int tiles = (int)((g.n_tiles - first + g.wgs - 1) / g.wgs); // of this workgroup: first, first + wgs, ...
-    f32x4 *const sums = reinterpret_cast<f32x4 *>(smem);              // [2][NW][MT][64]
-    uint8_t *const codes = smem + stream_sums(MT, NW);               // [blocks][rows][128], chunk c of a row at c ^ (row % 8)
+    const int blocks = (int)p.k_blocks, rows = (int)p.M;
+    const int64_t n_tiles = (p.N + 15) / 16;
+    const int tiles = (int)((n_tiles - blockIdx.x + gridDim.x - 1) / gridDim.x); // of this workgroup: its own number, and so on in steps of the grid
+    f32x4 *const sums = reinterpret_cast<f32x4 *>(smem);                         // [2][NW][64]
+    uint8_t *const codes = smem + stream_sums(NW);                               // [blocks][rows][128], chunk c of a row at c ^ (row % 8)
     float *const scales = reinterpret_cast<float *>(codes + (size_t)blocks * rows * kBlock); // [blocks][rows]
 
     struct Block {
@@ -97,7 +91,7 @@ __global__ __launch_bounds__(64 * NW) void stream_kernel(Product p, Stream g, OU
     int at_tile = 0, at_block = 0; // of the next request
     auto request = [&](Block &to) {
         if (at_tile >= tiles) return;
-        const int64_t n0 = 16 * (first + (int64_t)at_tile * g.wgs), kb = kb0 + wave + at_block * NW;
+        const int64_t n0 = 16 * (blockIdx.x + (int64_t)at_tile * gridDim.x), kb = wave + at_block * NW;
         const int n_last = (int)min(p.N - 1 - n0, (int64_t)15);
         const uint8_t *base = p.W + n0 * p.ldw + kb * kBlock;
         const uint32_t room = (uint32_t)min(p.ldw - kb * kBlock - 16, (int64_t)112), at = (uint32_t)min(row, n_last) * (uint32_t)p.ldw;
@@ -122,7 +116,7 @@ __global__ __launch_bounds__(64 * NW) void stream_kernel(Product p, Stream g, OU
 
     for (int i = threadIdx.x; i < blocks * rows * 8; i += 64 * NW) {
         const int chunk = i % 8, r = i / 8 % rows, kb = i / 8 / rows;
-        const int64_t k = (kb0 + kb) * kBlock + 16 * chunk;
+        const int64_t k = (int64_t)kb * kBlock + 16 * chunk;
         u32x4 v = {0, 0, 0, 0};
         if (k < p.K) v = *reinterpret_cast<const u32x4 *>(p.A + r * p.lda + k);
         if (k + 16 > p.K) {
@@ -131,61 +125,42 @@ __global__ __launch_bounds__(64 * NW) void stream_kernel(Product p, Stream g, OU
         }
         *reinterpret_cast<u32x4 *>(codes + (size_t)(kb * rows + r) * kBlock + 16 * (chunk ^ (r % 8))) = v;
     }
-    for (int i = threadIdx.x; i < blocks * rows; i += 64 * NW) scales[i] = p.SA[(kb0 + i / rows) * p.ldsa + i % rows];
+    for (int i = threadIdx.x; i < blocks * rows; i += 64 * NW) scales[i] = p.SA[i / rows * p.ldsa + i % rows];
     __syncthreads();
 
-    int r[MT];
-#pragma unroll
-    for (int i = 0; i < MT; ++i) r[i] = min(16 * i + row, rows - 1);
-    f32x4 acc[MT];
-    auto clear = [&] {
-#pragma unroll
-        for (int i = 0; i < MT; ++i) acc[i] = f32x4{0.f, 0.f, 0.f, 0.f};
-    };
-    clear();
+    const int r = min(row, rows - 1);
+    f32x4 acc = {0.f, 0.f, 0.f, 0.f};
     auto multiply = [&](Block &v, int block) {
-        const int64_t kb = kb0 + block;
-        if ((kb + 1) * kBlock > p.K) { // codes behind K
+        if ((int64_t)(block + 1) * kBlock > p.K) { // codes behind K
 #pragma unroll
             for (int h = 0; h < 2; ++h)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) v.w[h][e] &= kept((int)(p.K - (kb * kBlock + 16 * part + 64 * h + 4 * e)));
+                for (int e = 0; e < 4; ++e) v.w[h][e] &= kept((int)(p.K - ((int64_t)block * kBlock + 16 * part + 64 * h + 4 * e)));
         }
-        f16x8 w[4];
+        const uint8_t *c = codes + (size_t)(block * rows + r) * kBlock;
+        const u32x4 a[2] = {*reinterpret_cast<const u32x4 *>(c + 16 * (part ^ (r % 8))), *reinterpret_cast<const u32x4 *>(c + 16 * ((part + 4) ^ (r % 8)))};
+        f32x4 sum = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int e = 0; e < 4; ++e) w[e] = widened(v.w[e / 2][2 * (e % 2)], v.w[e / 2][2 * (e % 2) + 1]);
+        for (int e = 0; e < 4; ++e)
+            sum = __builtin_amdgcn_mfma_f32_16x16x32_f16(widened(v.w[e / 2][2 * (e % 2)], v.w[e / 2][2 * (e % 2) + 1]),
+                                                         widened(a[e / 2][2 * (e % 2)], a[e / 2][2 * (e % 2) + 1]), sum, 0, 0, 0);
+        const float sa = scales[block * rows + r];
 #pragma unroll
-        for (int i = 0; i < MT; ++i) {
-            const uint8_t *c = codes + (size_t)(block * rows + r[i]) * kBlock;
-            const u32x4 a[2] = {*reinterpret_cast<const u32x4 *>(c + 16 * (part ^ (r[i] % 8))),
-                                *reinterpret_cast<const u32x4 *>(c + 16 * ((part + 4) ^ (r[i] % 8)))};
-            f32x4 sum = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-                sum = __builtin_amdgcn_mfma_f32_16x16x32_f16(w[e], widened(a[e / 2][2 * (e % 2)], a[e / 2][2 * (e % 2) + 1]), sum, 0, 0, 0);
-            const float sa = scales[block * rows + r[i]];
-#pragma unroll
-            for (int e = 0; e < 4; ++e) acc[i][e] = __builtin_fmaf(sum[e], sa * v.sw[W1 ? e : 0], acc[i][e]);
-        }
+        for (int e = 0; e < 4; ++e) acc[e] = __builtin_fmaf(sum[e], sa * v.sw[W1 ? e : 0], acc[e]);
     };
     int tile = 0, block = 0;
     auto finish = [&] { // the tile is done: its sums of all waves, added by one of them
-        f32x4 *const mine = sums + (tile % 2) * (NW * MT * 64);
-#pragma unroll
-        for (int i = 0; i < MT; ++i) mine[(wave * MT + i) * 64 + lane] = acc[i];
+        f32x4 *const mine = sums + (tile % 2) * (NW * 64);
+        mine[wave * 64 + lane] = acc;
         __syncthreads();
-        for (int i = 0; i < MT; ++i) {
-            if ((tile * MT + i) % NW != wave) continue;
-            f32x4 sum = mine[i * 64 + lane];
+        if (tile % NW == wave) {
+            f32x4 sum = mine[lane];
 #pragma unroll
-            for (int w = 1; w < NW; ++w) sum += mine[(w * MT + i) * 64 + lane];
-            const int64_t m = 16 * i + row, n = 16 * (first + (int64_t)tile * g.wgs) + 4 * part;
-            if (m < p.M && n < p.N) {
-                if (g.slices > 1) store4(parts + ((int64_t)slice * p.M + m) * g.part_ld + n, sum, p.N - n);
-                else store4(C + m * p.ldc + n, sum, p.N - n);
-            }
+            for (int w = 1; w < NW; ++w) sum += mine[w * 64 + lane];
+            const int64_t n = 16 * (blockIdx.x + (int64_t)tile * gridDim.x) + 4 * part;
+            if (row < rows && n < p.N) store4(C + row * p.ldc + n, sum, p.N - n);
         }
-        clear();
+        acc = f32x4{0.f, 0.f, 0.f, 0.f};
         block = 0;
         ++tile;
     };
@@ -474,33 +449,25 @@ __global__ __launch_bounds__(256) void join_kernel(const float *parts, int split
     }
 }
 
-// How the kernel for few tokens splits a product; slices is 0 where the partial results do not fit the workspace.
-template <int MT, int NW>
-Stream plan_stream(const Product &p, size_t workspace_bytes)
+// Whether the kernel for few tokens takes a product: its tokens fit, and a workgroup has few enough tiles that their
+// barriers do not matter (57344 x 8192, 14 tiles each: 112 us, against 93 us by tiles through LDS; 28672 x 4096, 7 each: 29 against 29 to 31,
+// one token 27 against 29).  A product whose tokens do not fit is better off with tiles and splits along K (4096 x
+// 14336, sixteen tokens: 18 us, against 20 in two parts).
+constexpr int kStreamWaves = 16;
+bool few_tokens(const Product &p)
 {
-    Stream g;
-    g.n_tiles = ceil_div(p.N, 16);
-    g.part_ld = (p.N + 3) / 4 * 4;
-    const int64_t fit = (int64_t)((kLds - stream_sums(MT, NW)) / stream_block((int)p.M)); // blocks of K that LDS holds
-    g.per_slice = ceil_div(p.k_blocks, ceil_div(p.k_blocks, fit));
-    g.slices = (int)ceil_div(p.k_blocks, g.per_slice);
-    if (g.slices > 1 && workspace_bytes / 4 / (size_t)g.slices / (size_t)p.M < (size_t)g.part_ld) g.slices = 0;
-    else g.wgs = (int)std::min(g.n_tiles, std::max((int64_t)1, zs_compute_units() / (int64_t)g.slices));
-    return g;
+    return p.M <= 16 && stream_sums(kStreamWaves) + stream_block((int)p.M) * (size_t)p.k_blocks <= kLds &&
+           ceil_div(p.N, 16) <= 8 * (int64_t)zs_compute_units();
 }
 
-template <int MT, int NW, int D, bool W1, typename OUT>
-int run_stream(const Product &p, const Stream &g, OUT *C, void *workspace, hipStream_t s)
+template <bool W1, typename OUT>
+int run_stream(const Product &p, OUT *C, hipStream_t s)
 {
-    const int rc = allow_lds<stream_kernel<MT, NW, D, W1, OUT>>(kLds);
+    const int rc = allow_lds<stream_kernel<kStreamWaves, 2, W1, OUT>>(kLds);
     if (rc != ZS_OK) return rc;
-    const dim3 grid((unsigned)(g.slices * g.wgs));
-    const size_t lds = stream_sums(MT, NW) + stream_block((int)p.M) * (size_t)g.per_slice;
-    float *parts = static_cast<float *>(workspace);
-    hipLaunchKernelGGL((stream_kernel<MT, NW, D, W1, OUT>), grid, dim3(64 * NW), lds, s, p, g, C, parts);
-    if (g.slices > 1)
-        hipLaunchKernelGGL(join_kernel<OUT>, dim3(grid_for(ceil_div(p.M * g.part_ld / 4, 256))), dim3(256), 0, s, parts, g.slices, g.part_ld, C,
-                           p.ldc, p.M, p.N);
+    const dim3 grid((unsigned)std::min(ceil_div(p.N, 16), (int64_t)zs_compute_units()));
+    const size_t lds = stream_sums(kStreamWaves) + stream_block((int)p.M) * (size_t)p.k_blocks;
+    hipLaunchKernelGGL((stream_kernel<kStreamWaves, 2, W1, OUT>), grid, dim3(64 * kStreamWaves), lds, s, p, C);
     return launched();
 }
 
@@ -515,7 +482,7 @@ struct TileShape {
     int tokens, features;
     RoundTime alone[2], two[2];
 };
-constexpr TileShape kShapes[] = {{64, 128, {{1.5f, 0.81f}, {1.0f, 0.53f}}, {{2.7f, 1.08f}, {3.3f, 0.71f}}},
+constexpr TileShape kShapes[] = {{64, 128, {{1.5f, 0.81f}, {1.0f, 0.53f}}, {{2.7f, 1.17f}, {3.3f, 0.71f}}},
                                  {128, 128, {{3.4f, 1.05f}, {1.4f, 0.88f}}, {{4.5f, 1.95f}, {4.9f, 1.08f}}},
                                  {128, 128, {{}, {1.5f, 0.71f}}, {}}, // four blocks in LDS instead of two: fits once
                                  {256, 128, {{6.0f, 1.80f}, {3.6f, 1.14f}}, {}},
@@ -580,7 +547,7 @@ int run_tiled(const Product &p, OUT *C, void *workspace, size_t workspace_bytes,
     constexpr bool kExact = std::is_same_v<OUT, float>;
     const TilePlan plan = plan_tiles(p, kExact ? kFp32 : kBf16, workspace_bytes);
     switch (plan.shape) {
-    case 0: return run_tiles<4, 2, 1, 4, kExact ? 2 : 3>(p, plan.g, C, workspace, s);
+    case 0: return run_tiles<4, 2, 1, 4, 3>(p, plan.g, C, workspace, s);
     case 1: return run_tiles<2, 4, 4, 2, 2>(p, plan.g, C, workspace, s);
     case 3: return run_tiles<4, 4, 4, 2, kExact ? 2 : 3>(p, plan.g, C, workspace, s);
     default: break;
@@ -601,16 +568,8 @@ int run(const uint8_t *A, int64_t lda, const float *SA, int64_t ldsa, const uint
     if (lda > kMaxLd || ldw > kMaxLd) return ZS_ERR_SHAPE; // offsets inside a tile are 32 bits wide
     const Product p = {A, W, SA, SW, lda, ldsa, ldw, ldsw, ldc, M, N, K, ceil_div(K, kBlock), w_rows};
     hipStream_t stream = static_cast<hipStream_t>(hip_stream);
+    if (few_tokens(p)) return w_rows == 1 ? run_stream<true>(p, C, stream) : run_stream<false>(p, C, stream);
     if (!workspace) workspace_bytes = 0;
-    if (M <= 16) {
-        const Stream g = plan_stream<1, 16>(p, workspace_bytes);
-        if (g.slices)
-            return w_rows == 1 ? run_stream<1, 16, 2, true>(p, g, C, workspace, stream) : run_stream<1, 16, 2, false>(p, g, C, workspace, stream);
-    } else if (M <= 32) {
-        const Stream g = plan_stream<2, 16>(p, workspace_bytes);
-        if (g.slices)
-            return w_rows == 1 ? run_stream<2, 16, 2, true>(p, g, C, workspace, stream) : run_stream<2, 16, 2, false>(p, g, C, workspace, stream);
-    }
     return run_tiled(p, C, workspace, workspace_bytes, stream);
 }
 
