@@ -3,6 +3,8 @@
 #include "zs_device.h"
 #include "zs_ops.h"
 
+#include <algorithm>
+
 using namespace zs_ops;
 
 namespace {
@@ -21,7 +23,7 @@ __device__ __forceinline__ int64_t id_at(const void *ids, int id_bytes, int64_t 
 // plane bytes and the start of the FragTile that holds it.
 struct Blob {
     const uint8_t *bitmaps;
-    const uint32_t *offsets;
+    const u32x2 *offsets;
     const uint8_t *H;
     const uint8_t *L;
     uint64_t h_last, l_last; // offsets of the last byte of H and the last halfword of L: no read goes behind them
@@ -29,50 +31,62 @@ struct Blob {
     int32_t k_blocks;
 };
 
-__global__ __launch_bounds__(256) void embed_kernel(Blob b, int64_t N, const void *ids, int id_bytes, int64_t tasks, float scale,
-                                                    uint16_t *Y, int64_t ldy)
+template <int U> // BlockTiles whose planes a wave requests at a time
+__global__ __launch_bounds__(256) void embed_kernel(Blob b, int64_t N, const void *ids, int id_bytes, int64_t T, float scale, uint16_t *Y,
+                                                    int64_t ldy)
 {
-    const uint32_t lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
-    for (int64_t task = (int64_t)blockIdx.x * 4 + wave; task < tasks; task += (int64_t)gridDim.x * 4) {
-        const int64_t t = task / b.k_blocks, kb = task - t * b.k_blocks;
-        uint16_t *const out = Y + t * ldy + ZS_BT_DIM * kb + lane;
+    const uint32_t lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), j = lane % 8;
+    for (int64_t t = blockIdx.x; t < T; t += gridDim.x) {
         const int64_t id = id_at(ids, id_bytes, t, N);
-        if (id < 0) {
-            *out = 0;
-            continue;
-        }
-        const int64_t bt = id / ZS_BT_DIM * b.k_blocks + kb;
-        const uint32_t row = (uint32_t)(id % ZS_BT_DIM), r = row % 8;
+        const int64_t first = id < 0 ? 0 : id / ZS_BT_DIM * b.k_blocks;
+        const uint32_t row = (uint32_t)(id & (ZS_BT_DIM - 1)), r = row % 8;
         // column `lane`: FragTile column lane / 8, which lies in TensorCoreTile column lane / 32
-        const uint32_t f_row = row / 16 * ZS_FT_PER_TT + row / 8 % 2, j = lane % 8;
+        const uint32_t f_row = row / 16 * ZS_FT_PER_TT + row / 8 % 2;
         const uint32_t f = lane / 32 * (4 * ZS_FT_PER_TT) + lane / 8 % 4 * 2 + f_row, f_last = 4 * ZS_FT_PER_TT + 6 + f_row;
-        u32x2 p1 = {0, 0}, p2 = {0, 0}, p3 = {0, 0};
-        if (lane <= f_last) { // (the FragTiles behind the row's last one do not matter)
-            const u32x2 *planes = reinterpret_cast<const u32x2 *>(b.bitmaps + bt * ZS_BT_BITMAP_BYTES) + 3 * lane;
-            p1 = planes[0];
-            p2 = planes[1];
-            p3 = planes[2];
-        }
-        const uint64_t h_start = 16 * (uint64_t)b.offsets[2 * bt], l_start = 16 * (uint64_t)b.offsets[2 * bt + 1];
-        const uint32_t lo = p1.x | p2.x | p3.x, hi = p1.y | p2.y | p3.y;
         const uint64_t below = (1ull << (8 * r)) - 1; // of a FragTile, the rows above this one
-        const uint32_t count = __popc(lo) + __popc(hi);
-        const uint32_t start = zs::wave_inclusive_scan(count) - count + __popc(lo & (uint32_t)below) + __popc(hi & (uint32_t)(below >> 32));
-        const uint32_t at = 8 * (r % 4);
-        auto byte = [&](u32x2 p) { return (r < 4 ? p.x : p.y) >> at & 0xFFu; };
-        const uint32_t bytes = byte(p1) | byte(p2) << 8 | byte(p3) << 16;
-        const uint32_t w = (uint32_t)__shfl((int)bytes, (int)f), m = (w | w >> 8 | w >> 16) & 0xFFu;
-        const uint32_t h_at = (uint32_t)__shfl((int)start, (int)f) + __popc(m & ((1u << j) - 1u));
-        const uint32_t code = (w >> j & 1u) | (w >> (j + 8) & 1u) << 1 | (w >> (j + 16) & 1u) << 2;
-        uint32_t value;
-        if (code) {
-            const uint32_t h = b.H[min(h_start + h_at, b.h_last)];
-            value = (h & 0x80u) << 8 | ((uint32_t)(b.base_exp + (int)code) & 0xFFu) << 7 | (h & 0x7Fu);
-        } else {
-            const uint32_t l_at = 64 * f + 8 * r + j - h_at;
-            value = *reinterpret_cast<const uint16_t *>(b.L + min(l_start + 2 * l_at, b.l_last));
+        for (uint32_t kb0 = (blockIdx.y * 4 + wave) * U; kb0 < (uint32_t)b.k_blocks; kb0 += gridDim.y * 4 * U) {
+            uint16_t *const out = Y + t * ldy + ZS_BT_DIM * (int64_t)kb0 + lane;
+            if (id < 0) {
+#pragma unroll
+                for (int u = 0; u < U; ++u)
+                    if (kb0 + u < (uint32_t)b.k_blocks) out[ZS_BT_DIM * u] = 0;
+                continue;
+            }
+            u32x2 p[U][3], starts[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int64_t bt = first + min(kb0 + u, (uint32_t)b.k_blocks - 1);
+                const u32x2 *planes = reinterpret_cast<const u32x2 *>(b.bitmaps + bt * ZS_BT_BITMAP_BYTES) + 3 * lane;
+#pragma unroll
+                for (int i = 0; i < 3; ++i) p[u][i] = lane <= f_last ? planes[i] : u32x2{0, 0}; // (those behind the row's last one do not matter)
+                starts[u] = b.offsets[bt];
+            }
+            uint32_t value[U], code[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const uint32_t lo = p[u][0].x | p[u][1].x | p[u][2].x, hi = p[u][0].y | p[u][1].y | p[u][2].y;
+                const uint32_t count = __popc(lo) + __popc(hi);
+                const uint32_t start = zs::wave_inclusive_scan(count) - count + __popc(lo & (uint32_t)below) + __popc(hi & (uint32_t)(below >> 32));
+                const uint32_t at = 8 * (r % 4);
+                auto byte = [&](u32x2 v) { return (r < 4 ? v.x : v.y) >> at & 0xFFu; };
+                const uint32_t bytes = byte(p[u][0]) | byte(p[u][1]) << 8 | byte(p[u][2]) << 16;
+                const uint32_t w = (uint32_t)__shfl((int)bytes, (int)f), m = (w | w >> 8 | w >> 16) & 0xFFu;
+                const uint32_t h_at = (uint32_t)__shfl((int)start, (int)f) + __popc(m & ((1u << j) - 1u));
+                code[u] = (w >> j & 1u) | (w >> (j + 8) & 1u) << 1 | (w >> (j + 16) & 1u) << 2;
+                if (code[u]) {
+                    value[u] = b.H[min(16 * (uint64_t)starts[u].x + h_at, b.h_last)];
+                } else {
+                    const uint32_t l_at = 64 * f + 8 * r + j - h_at;
+                    value[u] = *reinterpret_cast<const uint16_t *>(b.L + min(16 * (uint64_t)starts[u].y + 2 * l_at, b.l_last));
+                }
+            }
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const uint32_t h = value[u];
+                const uint32_t bits = code[u] ? (h & 0x80u) << 8 | ((uint32_t)(b.base_exp + (int)code[u]) & 0xFFu) << 7 | (h & 0x7Fu) : h;
+                if (kb0 + u < (uint32_t)b.k_blocks) out[ZS_BT_DIM * u] = bf16_bits(bf16_value(bits) * scale);
+            }
         }
-        *out = bf16_bits(bf16_value(value) * scale);
     }
 }
 
@@ -358,16 +372,19 @@ extern "C" int zs_embed(const zs_desc *d, const void *blob_dev, const void *ids_
     const uint8_t *base = static_cast<const uint8_t *>(blob_dev);
     Blob b;
     b.bitmaps = base + d->off_bitmaps;
-    b.offsets = reinterpret_cast<const uint32_t *>(base + d->off_offsets);
+    b.offsets = reinterpret_cast<const u32x2 *>(base + d->off_offsets);
     b.H = d->h_bytes ? base + d->off_H : base; // (an empty section may lie at the blob's end)
     b.L = d->l_bytes ? base + d->off_L : base;
     b.h_last = d->h_bytes ? d->h_bytes - 1 : 0;
     b.l_last = d->l_bytes ? d->l_bytes - 2 : 0;
     b.base_exp = d->base_exp;
     b.k_blocks = (int32_t)(d->K / ZS_BT_DIM);
-    const int64_t tasks = T * b.k_blocks;
-    hipLaunchKernelGGL(embed_kernel, dim3(grid_for(ceil_div(tasks, 4))), dim3(256), 0, static_cast<hipStream_t>(hip_stream), b, d->N, ids_dev,
-                       id_bytes, tasks, scale, Y_dev, ldy);
+    // four BlockTiles to a wave, or one while that leaves fewer than 8192 waves
+    const int u = T * b.k_blocks >= 4 * 8192 ? 4 : 1;
+    const dim3 grid(grid_for(T), (unsigned)std::min(ceil_div(b.k_blocks, 4 * u), (int64_t)1024));
+    hipStream_t s = static_cast<hipStream_t>(hip_stream);
+    if (u == 4) hipLaunchKernelGGL(embed_kernel<4>, grid, dim3(256), 0, s, b, d->N, ids_dev, id_bytes, T, scale, Y_dev, ldy);
+    else hipLaunchKernelGGL(embed_kernel<1>, grid, dim3(256), 0, s, b, d->N, ids_dev, id_bytes, T, scale, Y_dev, ldy);
     return launched();
 }
 
