@@ -68,29 +68,22 @@ template <typename T, int ROWS, bool TRANSPOSE>
 __global__ __launch_bounds__(256) void quantize_tiles_kernel(const T *X, int64_t R, int64_t C, int64_t ldx, uint8_t *Q, int64_t ldq,
                                                              float *S, int64_t lds, int64_t c_tiles, int64_t tiles)
 {
-    constexpr int kPitch = kBlock + 16;
     __shared__ uint32_t peak[4][kBlock]; // by wave: of each column, or [0] of everything
-    __shared__ __attribute__((aligned(16))) uint8_t turned[TRANSPOSE ? kBlock * kPitch : 16];
+    __shared__ __attribute__((aligned(16))) uint8_t turned[TRANSPOSE ? kBlock * kBlock : 16]; // chunk c of column j at c ^ (j / 8 % 8)
     const int tid = threadIdx.x, wave = tid / 64, cg = tid % 16, rg = tid / 16;
     for (int64_t tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
         const int64_t rt = tile / c_tiles, ct = tile - rt * c_tiles;
         const int64_t r0 = rt * kBlock + 8 * rg, c0 = ct * kBlock + 8 * cg;
-        float v[8][8];
+        Eight<T> raw[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            if (r0 + i < R) {
-                load8(X + (r0 + i) * ldx + c0, C - c0, v[i]);
-            } else {
-#pragma unroll
-                for (int j = 0; j < 8; ++j) v[i][j] = 0.f;
-            }
-        }
+        for (int i = 0; i < 8; ++i) raw[i] = r0 + i < R ? fetch8(X + (r0 + i) * ldx + c0, C - c0) : Eight<T>{};
+        auto value = [&](int i, int j) { return value8(raw[i], j); };
         uint32_t a[8];
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
             a[j] = 0;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) a[j] = max(a[j], finite_magnitude(v[i][j]));
+            for (int i = 0; i < 8; ++i) a[j] = max(a[j], finite_magnitude(value(i, j)));
         }
         float inv[8];
         if constexpr (ROWS == kBlock) {
@@ -122,25 +115,24 @@ __global__ __launch_bounds__(256) void quantize_tiles_kernel(const T *X, int64_t
         }
         if constexpr (TRANSPOSE) {
 #pragma unroll
-            for (int j = 0; j < 8; ++j)
-                *reinterpret_cast<u32x2 *>(turned + (8 * cg + j) * kPitch + 8 * rg) =
-                    u32x2{codes4(v[0][j] * inv[j], v[1][j] * inv[j], v[2][j] * inv[j], v[3][j] * inv[j]),
-                          codes4(v[4][j] * inv[j], v[5][j] * inv[j], v[6][j] * inv[j], v[7][j] * inv[j])};
+            for (int j = 0; j < 8; ++j) {
+                auto q = [&](int i) { return codes4(value(i, j) * inv[j], value(i + 1, j) * inv[j], value(i + 2, j) * inv[j], value(i + 3, j) * inv[j]); };
+                *reinterpret_cast<u32x2 *>(turned + (8 * cg + j) * kBlock + 16 * ((rg / 2) ^ (cg % 8)) + 8 * (rg % 2)) = u32x2{q(0), q(4)};
+            }
             __syncthreads();
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const int c = 32 * i + tid / 8, at = 16 * (tid % 8);
                 if (ct * kBlock + c < C && rt * kBlock + at < R)
                     *reinterpret_cast<u32x4 *>(Q + (ct * kBlock + c) * ldq + rt * kBlock + at) =
-                        *reinterpret_cast<const u32x4 *>(turned + c * kPitch + at);
+                        *reinterpret_cast<const u32x4 *>(turned + c * kBlock + 16 * ((tid % 8) ^ (c / 8 % 8)));
             }
         } else {
 #pragma unroll
-            for (int i = 0; i < 8; ++i)
-                if (r0 + i < R && c0 < (C + 15) / 16 * 16)
-                    *reinterpret_cast<u32x2 *>(Q + (r0 + i) * ldq + c0) =
-                        u32x2{codes4(v[i][0] * inv[0], v[i][1] * inv[1], v[i][2] * inv[2], v[i][3] * inv[3]),
-                              codes4(v[i][4] * inv[4], v[i][5] * inv[5], v[i][6] * inv[6], v[i][7] * inv[7])};
+            for (int i = 0; i < 8; ++i) {
+                auto q = [&](int j) { return codes4(value(i, j) * inv[j], value(i, j + 1) * inv[j + 1], value(i, j + 2) * inv[j + 2], value(i, j + 3) * inv[j + 3]); };
+                if (r0 + i < R && c0 < (C + 15) / 16 * 16) *reinterpret_cast<u32x2 *>(Q + (r0 + i) * ldq + c0) = u32x2{q(0), q(4)};
+            }
         }
         __syncthreads(); // peak and turned are written again
     }
