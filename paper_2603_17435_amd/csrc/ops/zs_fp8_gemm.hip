@@ -13,7 +13,6 @@ namespace {
 
 constexpr int kBlock = 128;
 constexpr int64_t kMaxLd = (int64_t)1 << 23;
-constexpr int64_t kMaxTiles = (int64_t)1 << 22; // of one launch: its threads are counted in 32 bits
 
 struct Product {
     const uint8_t *A, *W;
@@ -530,7 +529,7 @@ template <int TM, int TN, int WM, int WN, int STAGES, typename OUT>
 int run_tiles(const Product &p, const Tiling &g, OUT *C, void *workspace, hipStream_t s)
 {
     constexpr bool kExact = std::is_same_v<OUT, float>;
-    if (g.tiles * g.splits > kMaxTiles) return ZS_ERR_SHAPE;
+    if (g.tiles * g.splits * (64 * WM * WN) > UINT32_MAX) return ZS_ERR_SHAPE; // (results of half a terabyte and more)
     float *parts = static_cast<float *>(workspace);
     const dim3 grid((unsigned)(g.tiles * g.splits)), wg(64 * WM * WN);
     if (p.w_rows == 1) hipLaunchKernelGGL((tiles_kernel<TM, TN, WM, WN, STAGES, true, kExact, OUT>), grid, wg, 0, s, p, g, C, parts);

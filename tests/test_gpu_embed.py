@@ -81,6 +81,27 @@ def test_packed_lookup_of_a_vocabulary():
     assert torch.equal(y, (w[ids].float() * 64).to(torch.bfloat16))
 
 
+def test_lookup_in_tables_of_more_than_4_gib():
+    import torch
+    n, k = 1 << 20, 4096
+    if torch.cuda.mem_get_info()[0] < 48 << 30:
+        pytest.skip("needs 48 GB")
+    gen = torch.Generator(device="cuda").manual_seed(2)
+    w = torch.empty(n, k, dtype=torch.bfloat16, device="cuda").normal_(0, 0.02, generator=gen)
+    ids = torch.tensor([n - 1, 0, 524288, 524287, n - 64, -1, 700001], device="cuda", dtype=torch.int32)
+    want = torch.where((ids >= 0)[:, None], w[ids.clamp_min(0).long()], torch.zeros((), dtype=torch.bfloat16, device="cuda"))
+    y = torch.empty(len(ids), k, dtype=torch.bfloat16, device="cuda")
+    binding.zs_dense_embed(w, n, k, ids, 4, len(ids), y)
+    assert torch.equal(y, want)
+    cap = binding.zs_encode_bound(n, k)
+    blob = torch.empty(cap, dtype=torch.uint8, device="cuda")
+    d = binding.zs_encode_device(w, n, k, blob, cap, torch.empty(binding.ZS_ENCODE_WORKSPACE_BYTES, dtype=torch.uint8, device="cuda"))
+    assert d.total_bytes > 1 << 32
+    y.fill_(7)
+    binding.zs_embed(d, blob, ids, 4, len(ids), y)
+    assert torch.equal(y, want)
+
+
 @pytest.mark.parametrize("n,k,ldw", [(1, 1, 1), (5, 7, 9), (100, 64, 64), (77, 129, 130), (300, 1000, 1008), (50, 2049, 2049)])
 def test_dense_lookup(n, k, ldw):
     rng = np.random.default_rng(k)
@@ -165,6 +186,29 @@ def test_grad_long_runs(t):
     for ids in (np.full(t, 3), np.full(t, -1), rng.integers(0, 2, t), np.sort(rng.integers(0, 9, t))[::-1].copy(),
                 rng.integers(0, 1 << 17, t) % 131, np.where(np.arange(t) % 32 < 31, 4, 2)):
         check_grad(ids.astype(np.int64), dy, 200)
+
+
+def test_no_tokens():
+    base = np.arange(12, dtype=np.float32).reshape(4, 3)
+    none = np.zeros(0, dtype=np.int64)
+    assert not gpu_grad(none, np.zeros((0, 3), dtype=np.float32), 4).any()
+    assert np.array_equal(gpu_grad(none, np.zeros((0, 3), dtype=np.float32), 4, base=base), base)
+
+
+def test_grad_of_padded_and_infinite_rows():
+    """What stands in a padded position does not reach the table; Inf and NaN reach their own row."""
+    t, n, k = 200, 20, 72
+    ids = np.arange(t) % 23 - 2                     # -2, -1 and 20 have no row
+    dy = np.ones((t, k), dtype=np.float32)
+    dy[(ids < 0) | (ids >= n)] = np.nan
+    dy[ids == 3] = np.inf
+    dy[np.nonzero(ids == 4)[0][1], 5] = np.nan
+    got = gpu_grad(ids, dy, n)
+    count = np.bincount(ids[(ids >= 0) & (ids < n)], minlength=n).astype(np.float32)
+    want = np.broadcast_to(count[:, None], (n, k)).copy()
+    want[3] = np.inf
+    want[4, 5] = np.nan
+    assert np.array_equal(got, want, equal_nan=True)
 
 
 def test_grad_of_a_large_table():

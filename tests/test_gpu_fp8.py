@@ -214,6 +214,45 @@ def test_gemm_on_another_stream():
     check_gemm(gpu_gemm(*args, 128, "bf16", stream=torch.cuda.Stream()), *args, 128, "bf16")
 
 
+def test_gemm_on_two_streams_at_a_time():
+    """Calls with a workspace each do not disturb one another."""
+    import torch
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    jobs = []
+    for i, (m, n, k) in enumerate([(40, 700, 3000), (300, 520, 2500)] * 3):
+        args = operands(m, n, k, 128, 50 + i)
+        a, w = dev(padded(args[0], up(k, 16), 0)), dev(padded(args[2], up(k, 16), 0))
+        jobs.append((args, a, dev(args[1]), w, dev(args[3]), torch.empty(m, n, device="cuda"), torch.empty(8 << 20, dtype=torch.uint8, device="cuda")))
+    torch.cuda.synchronize()
+    for _ in range(3):
+        for i, (args, a, sa, w, sw, c, ws) in enumerate(jobs):
+            binding.zs_fp8_gemm(a, sa, w, sw, c, a.shape[0], w.shape[0], args[0].shape[1], workspace_dev=ws, workspace_bytes=ws.numel(),
+                                stream=streams[i % 2])
+    torch.cuda.synchronize()
+    for args, *_, c, ws in jobs:
+        check_gemm(c.cpu().numpy(), *args, 128, "f32")
+
+
+@pytest.mark.parametrize("m,n,k,ldw", [(1, 32700, 100000, 140000), (2, 70000, 65500, 65536), (70, 70000, 65500, 65536)])
+def test_gemm_weights_of_more_than_4_gib(m, n, k, ldw):
+    """Small whole numbers again, so that sums of any order are exact; features from all over the matrix."""
+    import torch
+    if torch.cuda.mem_get_info()[0] < 24 << 30:
+        pytest.skip("needs 24 GB")
+    gen = torch.Generator(device="cuda").manual_seed(m)
+    codes = dev(ops.e4m3(np.arange(-4, 4)))
+    w = codes[torch.randint(0, 8, (n, ldw), generator=gen, device="cuda", dtype=torch.uint8).int()]
+    a = codes[torch.randint(0, 8, (m, ldw), generator=gen, device="cuda").int()]
+    kb = up(k, 128) // 128
+    sa, sw = torch.full((kb, m), 0.5, device="cuda"), torch.full((kb, up(n, 128) // 128), 2.0, device="cuda")
+    c = torch.empty(m, up(n, 4), device="cuda")
+    binding.zs_fp8_gemm(a, sa, w, sw, c, m, n, k, lda=ldw, ldw=ldw)
+    at = torch.tensor([0, 1, 12345, n // 2, 32767 if n > 40000 else 77, n - 130, n - 2, n - 1], device="cuda")
+    value = torch.float8_e4m3fn
+    ref = a[:, :k].view(value).double() @ w[at][:, :k].view(value).double().t()
+    assert torch.equal(c[:, at].double(), ref)
+
+
 # the layers of the benchmark, checked on sampled features (the oracle's time)
 @pytest.mark.parametrize("m,n,k", [(1, 1024, 4096), (16, 28672, 4096), (48, 4096, 14336), (200, 4096, 14336), (2048, 6144, 4096)])
 def test_gemm_layer_sizes(m, n, k):

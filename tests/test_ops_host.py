@@ -77,6 +77,8 @@ def test_gemm_refusals(fn):
         g(SHAPE, **{name: 0})
         g(SHAPE, **{name: -1})
         g(SHAPE, **{name: 1 << 31})
+    g(SHAPE, lda=(1 << 23) + 16)
+    g(SHAPE, ldw=(1 << 23) + 16)
     g(SHAPE, lda=288)
     g(SHAPE, lda=300)
     g(SHAPE, ldw=288)
