@@ -98,13 +98,7 @@ __global__ __launch_bounds__(256) void dense_embed_kernel(const uint16_t *W, int
     for (int64_t u = (int64_t)blockIdx.x * 256 + threadIdx.x; u < units; u += (int64_t)gridDim.x * 256) {
         const int64_t t = u / row_units, c = 8 * (u - t * row_units), left = K - c;
         const int64_t id = id_at(ids, id_bytes, t, N);
-        float v[8];
-        if (id >= 0) {
-            load8(W + id * ldw + c, left, v);
-        } else {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = 0.f;
-        }
+        const Values<uint16_t, 8> v = id >= 0 ? fetch<8>(W + id * ldw + c, left) : Values<uint16_t, 8>{};
         uint16_t *const out = Y + t * ldy + c;
         const float s = id >= 0 ? scale : 0.f;
         if (left >= 8) {
@@ -243,18 +237,14 @@ struct Runs {
     __device__ uint32_t id_behind(int64_t end) const { return end >= T ? kNoRow : id(end); }
 };
 
-constexpr int kCols = 8; // columns of a lane
+constexpr int kCols = 4; // columns of a lane: a wave's sums are whole lines
 
-__device__ __forceinline__ void put(float *p, const float v[kCols], int64_t left, float scale, bool add)
+__device__ __forceinline__ void put(float *p, f32x4 v, int64_t left, float scale, bool add)
 {
     if (left >= kCols) {
-        f32x4 a = {v[0] * scale, v[1] * scale, v[2] * scale, v[3] * scale}, b = {v[4] * scale, v[5] * scale, v[6] * scale, v[7] * scale};
-        if (add) {
-            a += load_any<f32x4>(p);
-            b += load_any<f32x4>(p + 4);
-        }
+        f32x4 a = {v[0] * scale, v[1] * scale, v[2] * scale, v[3] * scale};
+        if (add) a += load_any<f32x4>(p);
         store_any(p, a);
-        store_any(p + 4, b);
         return;
     }
 #pragma unroll
@@ -265,7 +255,7 @@ __device__ __forceinline__ void put(float *p, const float v[kCols], int64_t left
 template <typename T>
 __global__ __launch_bounds__(64) void sum_kernel(Runs g, const T *dY, int64_t lddy, float scale, float *dW, int64_t ldw, int add)
 {
-    constexpr int kAhead = sizeof(T) == 2 ? 16 : 8; // rows of dY requested at a time
+    constexpr int kAhead = 16; // rows of dY requested at a time
     for (int64_t task = blockIdx.x; task < g.chunks * g.slices; task += gridDim.x) {
         const int64_t chunk = task / g.slices, c = ((task - chunk * g.slices) * 64 + threadIdx.x) * kCols, left = g.K - c;
         const int64_t begin = chunk * g.chunk;
@@ -274,13 +264,13 @@ __global__ __launch_bounds__(64) void sum_kernel(Runs g, const T *dY, int64_t ld
         const Pair mine = g.pairs[begin + min((int)threadIdx.x, size - 1)];
         const uint32_t before = g.id_before(begin), behind = g.id_behind(begin + size);
         const int n = __builtin_popcountll(__builtin_amdgcn_ballot_w64((int)threadIdx.x < size && (uint32_t)(mine >> 32) != kNoRow));
-        float acc[kCols] = {};
+        f32x4 acc = {0.f, 0.f, 0.f, 0.f};
         for (int i0 = 0; i0 < n; i0 += kAhead) {
-            Eight<T> v[kAhead];
+            Values<T, kCols> v[kAhead];
 #pragma unroll
             for (int i = 0; i < kAhead; ++i) {
                 const int64_t t = (int64_t)(uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)mine, min(i0 + i, n - 1));
-                v[i] = fetch8(dY + t * lddy + c, left);
+                v[i] = fetch<kCols>(dY + t * lddy + c, left);
             }
 #pragma unroll
             for (int i = 0; i < kAhead; ++i) {
@@ -288,15 +278,14 @@ __global__ __launch_bounds__(64) void sum_kernel(Runs g, const T *dY, int64_t ld
                 if (at >= n) break;
                 const uint32_t id = (uint32_t)__builtin_amdgcn_readlane((int)(mine >> 32), at);
 #pragma unroll
-                for (int j = 0; j < kCols; ++j) acc[j] += value8(v[i], j);
+                for (int j = 0; j < kCols; ++j) acc[j] += v[i][j];
                 const uint32_t next = at + 1 < n ? (uint32_t)__builtin_amdgcn_readlane((int)(mine >> 32), at + 1) : behind;
                 if (at + 1 < n && next == id) continue;
                 // the run's sum over this chunk
                 if (id == before) put(g.heads + chunk * g.K + c, acc, left, 1.f, false);
                 else if (id == next) put(g.tails + chunk * g.K + c, acc, left, 1.f, false);
                 else put(dW + (int64_t)id * ldw + c, acc, left, scale, add);
-#pragma unroll
-                for (int j = 0; j < kCols; ++j) acc[j] = 0.f;
+                acc = f32x4{0.f, 0.f, 0.f, 0.f};
             }
         }
     }
@@ -311,17 +300,19 @@ __global__ __launch_bounds__(64) void join_kernel(Runs g, float scale, float *dW
         const int64_t begin = chunk * g.chunk, end = begin + g.chunk;
         const uint32_t id = g.id(end - 1);
         if (id == kNoRow || id != g.id(end) || id == g.id_before(begin)) continue;
-        float acc[kCols];
-        load8(g.tails + chunk * g.K + c, left, acc);
+        f32x4 acc;
+        const Values<float, kCols> tail = fetch<kCols>(g.tails + chunk * g.K + c, left);
+#pragma unroll
+        for (int j = 0; j < kCols; ++j) acc[j] = tail[j];
         for (int64_t k = chunk + 1; k < g.chunks;) {
             // of the next 64 chunks, those that begin inside the run: the first ones
             const int64_t mine = k + threadIdx.x;
             const uint64_t inside = __builtin_amdgcn_ballot_w64(mine < g.chunks && g.id(min(mine, g.chunks - 1) * g.chunk) == id);
             const int n = inside == ~0ull ? 64 : __builtin_ctzll(~inside);
             for (int i0 = 0; i0 < n; i0 += kAhead) {
-                float v[kAhead][kCols];
+                Values<float, kCols> v[kAhead];
 #pragma unroll
-                for (int i = 0; i < kAhead; ++i) load8(g.heads + (k + min(i0 + i, n - 1)) * g.K + c, left, v[i]);
+                for (int i = 0; i < kAhead; ++i) v[i] = fetch<kCols>(g.heads + (k + min(i0 + i, n - 1)) * g.K + c, left);
 #pragma unroll
                 for (int i = 0; i < kAhead; ++i)
                     if (i0 + i < n)
@@ -344,9 +335,9 @@ GradPlan plan_grad(int64_t T, int64_t K)
 {
     GradPlan p;
     auto up = [](size_t x) { return (x + 255) / 256 * 256; };
-    // 32 tokens to a chunk where that makes 1024 waves or more, else 8: more waves, more partial sums
+    // 32 tokens to a chunk where that makes 1024 waves or more, else 16, or 8 of a small dY: more waves, more partial sums
     p.slices = ceil_div(K, 64 * kCols);
-    p.chunk = ceil_div(T, 32) * p.slices >= 1024 ? 32 : 8;
+    p.chunk = ceil_div(T, 32) * p.slices >= 1024 ? 32 : T * K > 1 << 20 ? 16 : 8;
     p.chunks = ceil_div(T, p.chunk);
     p.pairs_bytes = up(8 * (size_t)T);
     p.sums_bytes = up(4 * (size_t)p.chunks * (size_t)K);

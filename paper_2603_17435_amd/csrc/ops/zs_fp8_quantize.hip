@@ -47,8 +47,7 @@ __global__ __launch_bounds__(256) void quantize_rows_kernel(const T *X, int64_t 
     const int64_t blocks = R * k_blocks, step = (int64_t)gridDim.x * 16;
     for (int64_t b = (int64_t)blockIdx.x * 16 + threadIdx.x / 16; b < blocks; b += step) {
         const int64_t r = b / k_blocks, kb = b - r * k_blocks, c = kb * kBlock + 8 * (threadIdx.x % 16);
-        float v[8];
-        load8(X + r * ldx + c, C - c, v);
+        const Values<T, 8> v = fetch<8>(X + r * ldx + c, C - c);
         uint32_t a = 0;
 #pragma unroll
         for (int i = 0; i < 8; ++i) a = max(a, finite_magnitude(v[i]));
@@ -74,10 +73,10 @@ __global__ __launch_bounds__(256) void quantize_tiles_kernel(const T *X, int64_t
     for (int64_t tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
         const int64_t rt = tile / c_tiles, ct = tile - rt * c_tiles;
         const int64_t r0 = rt * kBlock + 8 * rg, c0 = ct * kBlock + 8 * cg;
-        Eight<T> raw[8];
+        Values<T, 8> raw[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) raw[i] = r0 + i < R ? fetch8(X + (r0 + i) * ldx + c0, C - c0) : Eight<T>{};
-        auto value = [&](int i, int j) { return value8(raw[i], j); };
+        for (int i = 0; i < 8; ++i) raw[i] = r0 + i < R ? fetch<8>(X + (r0 + i) * ldx + c0, C - c0) : Values<T, 8>{};
+        auto value = [&](int i, int j) { return raw[i][j]; };
         uint32_t a[8];
 #pragma unroll
         for (int j = 0; j < 8; ++j) {

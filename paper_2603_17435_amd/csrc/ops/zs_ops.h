@@ -44,36 +44,28 @@ __device__ __forceinline__ uint32_t bf16_pair(float lo, float hi)
     return __builtin_bit_cast(uint32_t, bf16x2{(__bf16)lo, (__bf16)hi});
 }
 
-// Eight consecutive values of a row of BF16 patterns or floats as they lie there; those at and behind `left` are zero.
-template <typename T>
-struct Eight {
-    u32x4 w[sizeof(T) / 2];
+// N consecutive values of a row of BF16 patterns or floats as they lie there; those at and behind `left` are zero.
+template <typename T, int N>
+struct Values {
+    uint32_t w[N * sizeof(T) / 4];
+    __device__ __forceinline__ float operator[](int i) const // i is a constant
+    {
+        const uint32_t v = w[i * (int)sizeof(T) / 4];
+        return __builtin_bit_cast(float, sizeof(T) == 4 ? v : i % 2 ? v & 0xFFFF0000u : v << 16);
+    }
 };
-template <typename T>
-__device__ __forceinline__ Eight<T> fetch8(const T *p, int64_t left)
+template <int N, typename T>
+__device__ __forceinline__ Values<T, N> fetch(const T *p, int64_t left)
 {
-    if (left >= 8) return load_any<Eight<T>>(p);
-    Eight<T> e = {};
+    if (left >= N) return load_any<Values<T, N>>(p);
+    Values<T, N> v = {};
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
+    for (int i = 0; i < N; ++i)
         if (i < left) {
-            if constexpr (sizeof(T) == 2) e.w[0][i / 2] |= (uint32_t)p[i] << (16 * (i % 2));
-            else e.w[i / 4][i % 4] = __builtin_bit_cast(uint32_t, p[i]);
+            if constexpr (sizeof(T) == 2) v.w[i / 2] |= (uint32_t)p[i] << (16 * (i % 2));
+            else v.w[i] = __builtin_bit_cast(uint32_t, p[i]);
         }
-    return e;
-}
-template <typename T>
-__device__ __forceinline__ float value8(const Eight<T> &e, int i) // i is a constant
-{
-    const uint32_t w = sizeof(T) == 2 ? e.w[0][i / 2] : e.w[(i / 4) % (sizeof(T) / 2)][i % 4];
-    return __builtin_bit_cast(float, sizeof(T) == 4 ? w : i % 2 ? w & 0xFFFF0000u : w << 16);
-}
-template <typename T>
-__device__ __forceinline__ void load8(const T *p, int64_t left, float v[8])
-{
-    const Eight<T> e = fetch8(p, left);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = value8(e, i);
+    return v;
 }
 
 inline bool aligned(const void *p, uintptr_t to) { return reinterpret_cast<uintptr_t>(p) % to == 0; }
