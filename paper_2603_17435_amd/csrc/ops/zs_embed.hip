@@ -20,7 +20,9 @@ __device__ __forceinline__ int64_t id_at(const void *ids, int id_bytes, int64_t 
 // A wave decodes one token's 64 weights of one BlockTile.  Lane f first stands for FragTile f: where the
 // row's bytes of a FragTile start in H is the number of in-window elements before them, which a prefix sum of the popcounts
 // over the lanes gives.  Then lane c stands for the row's column c and fetches the three
-// plane bytes and the start of the FragTile that holds it.
+// plane bytes and the start of the FragTile that holds it.  Per BlockTile 40 to 64 FragTiles' planes of 24 bytes and 64 to 128
+// bytes of the row are read: 5000 frequent and rare tokens of 128256 x 4096 take 81 us, with 151 MB from memory and as much again
+// from the caches.  Bound by latency (32 tokens: 2.9 us) and instructions below that.
 struct Blob {
     const uint8_t *bitmaps;
     const u32x2 *offsets;
@@ -91,7 +93,7 @@ __global__ __launch_bounds__(256) void embed_kernel(Blob b, int64_t N, const voi
 }
 
 // ---- rows of a BF16 table ------------------------------------------------------------------
-// A thread takes eight columns of one token.
+// A thread takes eight columns of one token.  Bound by memory: 16384 tokens of 128256 x 4096 take 48 us (268 MB both ways, 5.6 TB/s).
 __global__ __launch_bounds__(256) void dense_embed_kernel(const uint16_t *W, int64_t N, int64_t K, int64_t ldw, const void *ids, int id_bytes,
                                                           int64_t units, int64_t row_units, float scale, uint16_t *Y, int64_t ldy)
 {
@@ -166,7 +168,9 @@ __device__ __forceinline__ uint32_t partner(uint32_t x, int d)
     }
 }
 
-// Sorts kTile pairs in each of the first `tiles` workgroups; the others clear their part of dW meanwhile.
+// Sorts kTile pairs in each of the first `tiles` workgroups; the others clear their part of dW meanwhile.  The sorting is bound by
+// the latency of the network's 55 steps, ten of them through LDS (7.5 us with 509 pairs), and so hidden by a large dW (140 us for
+// half of 128256 x 4096, 7 TB/s).
 __global__ __launch_bounds__(kTile) void sort_tiles_kernel(const void *ids, int id_bytes, int64_t T, int64_t N, Pair *out, int tiles, Zeros z)
 {
     __shared__ Pair keys[kTile];
@@ -253,6 +257,8 @@ __device__ __forceinline__ void put(float *p, f32x4 v, int64_t left, float scale
         if (i < left) p[i] = add ? p[i] + v[i] * scale : v[i] * scale;
 }
 
+// Sums of a chunk.  Bound by memory with many tokens: 16384 of 4096 BF16 columns take 53 us (134 MB read, a row of dW written for each id); by the
+// latency of one round of loads with few (509 tokens of 1024 columns: 4 us).
 template <typename T>
 __global__ __launch_bounds__(64) void sum_kernel(Runs g, const T *dY, int64_t lddy, float scale, float *dW, int64_t ldw, int add)
 {
@@ -292,38 +298,76 @@ __global__ __launch_bounds__(64) void sum_kernel(Runs g, const T *dY, int64_t ld
     }
 }
 
-// Runs over several chunks: the chunk in which one begins adds up what the chunks behind it left, in their order.
-__global__ __launch_bounds__(64) void join_kernel(Runs g, float scale, float *dW, int64_t ldw, int add)
+// Runs over several chunks: what the chunks behind its first one left is added up in their order.  A wave takes the run
+// that begins in one chunk, if any does; a workgroup has the runs of eight neighbouring chunks, of which one at most is
+// longer than sixteen, and its waves share that one: each adds sixteen chunks in turn, then the waves are added in order.
+// (A wave by itself for each run: 112 instead of 78 us for a call with 16384 tokens of one id, K = 4096, and the same for others.)
+constexpr int kJoinWaves = 8, kJoinAhead = 16;
+
+__device__ __forceinline__ void add_heads(f32x4 &acc, const Runs &g, int64_t from, int n, int64_t c, int64_t left)
 {
-    constexpr int kAhead = 16;
-    for (int64_t task = blockIdx.x; task < (g.chunks - 1) * g.slices; task += gridDim.x) {
-        const int64_t chunk = task / g.slices, c = ((task - chunk * g.slices) * 64 + threadIdx.x) * kCols, left = g.K - c;
-        const int64_t begin = chunk * g.chunk, end = begin + g.chunk;
-        const uint32_t id = g.id(end - 1);
-        if (id == kNoRow || id != g.id(end) || id == g.id_before(begin)) continue;
-        f32x4 acc;
-        const Values<float, kCols> tail = fetch<kCols>(g.tails + chunk * g.K + c, left);
+    Values<float, kCols> v[kJoinAhead];
 #pragma unroll
-        for (int j = 0; j < kCols; ++j) acc[j] = tail[j];
-        for (int64_t k = chunk + 1; k < g.chunks;) {
-            // of the next 64 chunks, those that begin inside the run: the first ones
-            const int64_t mine = k + threadIdx.x;
-            const uint64_t inside = __builtin_amdgcn_ballot_w64(mine < g.chunks && g.id(min(mine, g.chunks - 1) * g.chunk) == id);
-            const int n = inside == ~0ull ? 64 : __builtin_ctzll(~inside);
-            for (int i0 = 0; i0 < n; i0 += kAhead) {
-                Values<float, kCols> v[kAhead];
+    for (int i = 0; i < kJoinAhead; ++i) v[i] = fetch<kCols>(g.heads + (from + min(i, n - 1)) * g.K + c, left);
 #pragma unroll
-                for (int i = 0; i < kAhead; ++i) v[i] = fetch<kCols>(g.heads + (k + min(i0 + i, n - 1)) * g.K + c, left);
+    for (int i = 0; i < kJoinAhead; ++i)
+        if (i < n)
 #pragma unroll
-                for (int i = 0; i < kAhead; ++i)
-                    if (i0 + i < n)
-#pragma unroll
-                        for (int j = 0; j < kCols; ++j) acc[j] += v[i][j];
+            for (int j = 0; j < kCols; ++j) acc[j] += v[i][j];
+}
+
+__global__ __launch_bounds__(64 * kJoinWaves) void join_kernel(Runs g, float scale, float *dW, int64_t ldw, int add)
+{
+    __shared__ f32x4 sums[kJoinWaves][64];
+    __shared__ int shared_run; // the wave that found the run for all of them
+    const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+    const int64_t groups = (g.chunks - 1 + kJoinWaves - 1) / kJoinWaves;
+    for (int64_t task = blockIdx.x; task < groups * g.slices; task += gridDim.x) {
+        const int64_t group = task / g.slices, first = group * kJoinWaves, c = ((task - group * g.slices) * 64 + lane) * kCols, left = g.K - c;
+        auto tail = [&](int64_t chunk) {
+            const Values<float, kCols> v = fetch<kCols>(g.tails + chunk * g.K + c, left);
+            return f32x4{v[0], v[1], v[2], v[3]};
+        };
+        auto inside = [&](int64_t k, uint32_t id) { // of the chunks from k on, how many begin inside the run (up to kJoinAhead + 1)
+            const uint64_t begin = __builtin_amdgcn_ballot_w64(lane <= kJoinAhead && k + lane < g.chunks && g.id(min(k + lane, g.chunks - 1) * g.chunk) == id);
+            return (int)__builtin_ctzll(~begin);
+        };
+        if (threadIdx.x == 0) shared_run = -1;
+        __syncthreads();
+        const int64_t chunk = first + wave;
+        if (chunk + 1 < g.chunks) {
+            const int64_t begin = chunk * g.chunk, end = begin + g.chunk;
+            const uint32_t id = g.id(end - 1);
+            if (id != kNoRow && id == g.id(end) && id != g.id_before(begin)) {
+                const int n = inside(chunk + 1, id);
+                if (n > kJoinAhead) {
+                    if (lane == 0) shared_run = wave;
+                } else {
+                    f32x4 acc = tail(chunk);
+                    add_heads(acc, g, chunk + 1, n, c, left);
+                    put(dW + (int64_t)id * ldw + c, acc, left, scale, add);
+                }
             }
-            if (n < 64) break;
-            k += 64;
         }
-        put(dW + (int64_t)id * ldw + c, acc, left, scale, add);
+        __syncthreads();
+        const int run = __builtin_amdgcn_readfirstlane(shared_run);
+        if (run < 0) continue;
+        const uint32_t id = g.id((first + run + 1) * g.chunk - 1);
+        f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+        if (wave == 0) acc = tail(first + run);
+        for (int64_t k = first + run + 1 + kJoinAhead * wave;; k += kJoinAhead * kJoinWaves) {
+            const int n = min(inside(k, id), kJoinAhead);
+            if (n > 0) add_heads(acc, g, k, n, c, left);
+            if (n < kJoinAhead) break;
+        }
+        sums[wave][lane] = acc;
+        __syncthreads();
+        if (wave == 0) {
+#pragma unroll
+            for (int w = 1; w < kJoinWaves; ++w) acc += sums[w][lane];
+            put(dW + (int64_t)id * ldw + c, acc, left, scale, add);
+        }
+        __syncthreads();
     }
 }
 
@@ -336,9 +380,10 @@ GradPlan plan_grad(int64_t T, int64_t K)
 {
     GradPlan p;
     auto up = [](size_t x) { return (x + 255) / 256 * 256; };
-    // 32 tokens to a chunk where that makes 1024 waves or more, else 16, or 8 of a small dY: more waves, more partial sums
     p.slices = ceil_div(K, 64 * kCols);
-    p.chunk = ceil_div(T, 32) * p.slices >= 1024 ? 32 : T * K > 1 << 20 ? 16 : 8;
+    // Small chunks make more waves, and more partial sums.  With 8, 16 and 32 tokens, us: 256 tokens x 4096 columns 14, 16, 22;
+    // 512 17, 19, 25; 4096 55, 54, 58; 16384 137, 127, 121 (frequent ids) or 102, 84, 78 (one id).
+    p.chunk = T * K <= 1 << 21 ? 8 : T * K < 1 << 25 ? 16 : 32;
     p.chunks = ceil_div(T, p.chunk);
     p.pairs_bytes = up(8 * (size_t)T);
     p.sums_bytes = up(4 * (size_t)p.chunks * (size_t)K);
@@ -371,7 +416,8 @@ extern "C" int zs_embed(const zs_desc *d, const void *blob_dev, const void *ids_
     b.l_last = d->l_bytes ? d->l_bytes - 2 : 0;
     b.base_exp = d->base_exp;
     b.k_blocks = (int32_t)(d->K / ZS_BT_DIM);
-    // four BlockTiles to a wave, or one while that leaves fewer than 8192 waves
+    // Four BlockTiles to a wave, or one while that leaves fewer than 8192 waves.  K = 4096, one against four, us: 32 tokens 2.9
+    // and 3.9, 256 8.8 and 9.2, 512 14.9 and 14.5, 2048 45 and 43; 5000 of which many are cached 106 and 81, 8192 of which few are 144 and 157.
     const int u = T * b.k_blocks >= 4 * 8192 ? 4 : 1;
     const dim3 grid(grid_for(T), (unsigned)std::min(ceil_div(b.k_blocks, 4 * u), (int64_t)1024));
     hipStream_t s = static_cast<hipStream_t>(hip_stream);
@@ -455,6 +501,6 @@ extern "C" int zs_embed_grad(const void *ids_dev, int id_bytes, int64_t T, const
         hipLaunchKernelGGL(sum_kernel<uint16_t>, grid, dim3(64), 0, s, g, static_cast<const uint16_t *>(dY_dev), lddy, scale, dW_dev, lddw, accumulate);
     else
         hipLaunchKernelGGL(sum_kernel<float>, grid, dim3(64), 0, s, g, static_cast<const float *>(dY_dev), lddy, scale, dW_dev, lddw, accumulate);
-    if (g.chunks > 1) hipLaunchKernelGGL(join_kernel, dim3(grid_for((g.chunks - 1) * g.slices)), dim3(64), 0, s, g, scale, dW_dev, lddw, accumulate);
+    if (g.chunks > 1) hipLaunchKernelGGL(join_kernel, dim3(grid_for(ceil_div(g.chunks - 1, kJoinWaves) * g.slices)), dim3(64 * kJoinWaves), 0, s, g, scale, dW_dev, lddw, accumulate);
     return launched();
 }

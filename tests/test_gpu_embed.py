@@ -188,6 +188,17 @@ def test_grad_long_runs(t):
         check_grad(ids.astype(np.int64), dy, 200)
 
 
+@pytest.mark.parametrize("t,k", [(6000, 5), (6000, 300), (12000, 1000)])
+def test_grad_runs_of_every_length(t, k):
+    """Runs of less and more than sixteen chunks (of 8 or 16 tokens), which begin at each place of a workgroup's eight chunks."""
+    lengths = [3, 16, 33, 136, 137, 1, 150, 270, 290, 64, 8 * 129 + 3, 5, 300, 7, 1500, 129, 128, 2, 145]
+    ids = np.concatenate([np.full(n, 2 * i) for i, n in enumerate(lengths * 3)])[:t]
+    rng = np.random.default_rng(k)
+    dy = rng.standard_normal((t, k)).astype(np.float32)
+    ids = np.concatenate([ids, np.full(t - len(ids), -1)])
+    check_grad(rng.permutation(ids), dy, 120, 0.5)
+
+
 def test_no_tokens():
     base = np.arange(12, dtype=np.float32).reshape(4, 3)
     none = np.zeros(0, dtype=np.int64)
