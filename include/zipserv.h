@@ -356,7 +356,7 @@ int zs_fp8_gemm_bf16(const uint8_t *A_dev, int64_t lda, const float *SA_dev, int
  *   ids_dev  T ids of id_bytes 4 (int32_t) or 8 (int64_t) each, naturally aligned    (device, in)
  *            An id that is negative or not below the table's number of rows marks a padded
  *            position: its row of Y is zero, and it takes no part in the gradient.
- *   T        >= 0; with no tokens the other device pointers may be NULL */
+ *   T        >= 0; with no tokens ids_dev, Y_dev, dY_dev and workspace_dev may be NULL */
 
 /* Y[t] = bf16(scale * decode(W)[ids[t]]), the product in FP32, rounded once.
  *   blob_dev  the encoded table, 256-byte aligned                                    (device, in)
