@@ -128,9 +128,9 @@ int check_lookup(const void *ids, int id_bytes, int64_t T, const void *Y, int64_
 // a chunk's rows of dY over a slice of the columns.  A run of one id that lies inside a chunk is finished
 // there; one that crosses a boundary leaves a partial sum for each chunk in the workspace, and these are added in order.
 // Every sum has one fixed order: the result is the same from run to run.
-constexpr int kTile = 1024; // pairs sorted by one workgroup
+constexpr int kTile = 1024; // pairs sorted by one workgroup, a thread each
 constexpr int kFan = 16;    // sorted lists merged at a time
-constexpr uint32_t kNoRow = 0xFFFFFFFFu;
+constexpr uint32_t kNoRow = 0x7FFFFFFFu; // (a table has fewer rows)
 
 typedef uint64_t Pair; // id << 32 | position: all different, so that a pair's place is a count of smaller ones
 
@@ -142,16 +142,83 @@ struct Zeros {
     float *p;
     int64_t rows, cols, ld;
 };
+// A workgroup has a store of 16 bytes for each thread: a part of a row, or several short rows side by side.  With stores in a loop
+// 2 GB take 440 to 570 us (1024 to 8192 workgroups of 256 threads) instead of 300.
+struct Clearing {
+    int64_t units, across, side, wgs; // stores to a row, workgroups across a row, rows side by side, workgroups for everything
+};
+__host__ __device__ __forceinline__ Clearing clearing(const Zeros &z, int threads)
+{
+    Clearing c;
+    c.units = (z.cols + 3) / 4;
+    c.across = (c.units + threads - 1) / threads;
+    c.side = z.rows > 1 && c.units < threads ? threads / c.units : 1;
+    c.wgs = c.side > 1 ? (z.rows + c.side - 1) / c.side : z.rows * c.across;
+    return c;
+}
+template <int THREADS>
 __device__ __forceinline__ void clear(const Zeros &z, int64_t wg, int64_t wgs)
 {
-    const int64_t across = z.rows == 1 ? wgs : 1; // workgroups that share a row
-    for (int64_t r = z.rows == 1 ? 0 : wg; r < z.rows; r += wgs)
-        for (int64_t c = 4 * ((z.rows == 1 ? wg * blockDim.x : 0) + threadIdx.x); c < z.cols; c += 4 * across * blockDim.x) {
-            float *q = z.p + r * z.ld + c;
-            if (c + 4 <= z.cols) __builtin_nontemporal_store(f32x4{0.f, 0.f, 0.f, 0.f}, reinterpret_cast<f32x4_any *>(q));
-            else
-                for (int64_t i = 0; i < z.cols - c; ++i) q[i] = 0.f;
+    const Clearing plan = clearing(z, THREADS);
+    uint32_t at = threadIdx.x, beside = 0;
+    if (plan.side > 1) {
+        beside = at / (uint32_t)plan.units;
+        at -= beside * (uint32_t)plan.units;
+        if (beside >= plan.side) return;
+    }
+    for (; wg < plan.wgs; wg += wgs) {
+        const int64_t row = z.rows == 1 ? 0 : plan.across == 1 ? wg * plan.side + beside : wg / plan.across;
+        const int64_t u = plan.across == 1 ? at : at + (wg - row * plan.across) * THREADS;
+        if (row >= z.rows || u >= plan.units) continue;
+        float *q = z.p + row * z.ld + 4 * u;
+        if (4 * u + 4 <= z.cols) __builtin_nontemporal_store(f32x4{0.f, 0.f, 0.f, 0.f}, reinterpret_cast<f32x4_any *>(q));
+        else
+            for (int64_t i = 0; i < z.cols - 4 * u; ++i) q[i] = 0.f;
+    }
+}
+
+// Up to kCounted pairs: a pair's place is the number of smaller ones.  Sixteen lanes to a pair, which compare it with four ids each at
+// a time, in the first `wgs` workgroups; the others clear dW meanwhile.  Bound by latency for few pairs, then by the T^2 comparisons.  Whole calls with
+// 1024 BF16 columns added to dW, counted against sorted and merged, us: 64 tokens 9.5 and 13.8, 2048 17 and 23, 4096 28 and 30, 6000 33 and 32.
+constexpr int kCounted = 4096;
+__global__ __launch_bounds__(256) void count_kernel(const void *ids, int id_bytes, int T, int64_t N, Pair *out, int wgs, Zeros z)
+{
+    extern __shared__ __attribute__((aligned(16))) uint32_t keys[];
+    if ((int)blockIdx.x >= wgs) {
+        clear<256>(z, blockIdx.x - wgs, gridDim.x - wgs);
+        return;
+    }
+    const int blocks = (T + 63) / 64, tid = threadIdx.x, lane = tid % kFan;
+    for (int i = tid; i < 64 * blocks; i += 256) {
+        uint32_t key = ~0u; // behind the last: larger than any
+        if (i < T) {
+            const int64_t id = id_at(ids, id_bytes, i, N);
+            key = id < 0 ? kNoRow : (uint32_t)id;
         }
+        keys[i] = key;
+    }
+    __syncthreads();
+    const int t = blockIdx.x * (256 / kFan) + tid / kFan, own = blockIdx.x * (256 / kFan) / 64; // the block of 64 ids with this workgroup's pairs
+    const uint32_t mine = keys[t];
+    int smaller = 0;
+    auto ids_of = [&](int b) { return *reinterpret_cast<const u32x4 *>(keys + 64 * b + 4 * lane); };
+#pragma unroll 4
+    for (int b = 0; b < own; ++b) { // earlier positions
+        const u32x4 v = ids_of(b);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) smaller += v[e] <= mine;
+    }
+    const u32x4 v = ids_of(own);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) smaller += v[e] < mine + (64 * own + 4 * lane + e < t);
+#pragma unroll 4
+    for (int b = own + 1; b < blocks; ++b) {
+        const u32x4 w = ids_of(b);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) smaller += w[e] < mine;
+    }
+    for (int d = 1; d < kFan; d *= 2) smaller += __shfl_xor(smaller, d);
+    if (lane == 0 && t < T) out[smaller] = (Pair)mine << 32 | (uint32_t)t;
 }
 
 // The value of the lane whose number differs in bit d (a constant): within a row of sixteen lanes by moves of the
@@ -169,14 +236,13 @@ __device__ __forceinline__ uint32_t partner(uint32_t x, int d)
 }
 
 // Sorts kTile pairs in each of the first `tiles` workgroups; the others clear their part of dW meanwhile.  The sorting is bound by
-// the latency of the network's 55 steps, ten of them through LDS (7.5 us with 509 pairs), and so hidden by a large dW (140 us for
-// half of 128256 x 4096, 7 TB/s).
+// the latency of the network's 55 steps, ten of them through LDS (7.5 us).
 __global__ __launch_bounds__(kTile) void sort_tiles_kernel(const void *ids, int id_bytes, int64_t T, int64_t N, Pair *out, int tiles, Zeros z)
 {
     __shared__ Pair keys[kTile];
     const int tid = threadIdx.x;
     if ((int)blockIdx.x >= tiles) {
-        clear(z, blockIdx.x - tiles, gridDim.x - tiles);
+        clear<kTile>(z, blockIdx.x - tiles, gridDim.x - tiles);
         return;
     }
     const int64_t t = (int64_t)blockIdx.x * kTile + tid;
@@ -225,7 +291,7 @@ __device__ __forceinline__ void merge(const Pair *in, Pair *out, int64_t T, int6
 __global__ __launch_bounds__(256) void merge_kernel(const Pair *in, Pair *out, int64_t T, int64_t run, int wgs, Zeros z)
 {
     if ((int)blockIdx.x >= wgs) {
-        clear(z, blockIdx.x - wgs, gridDim.x - wgs);
+        clear<256>(z, blockIdx.x - wgs, gridDim.x - wgs);
         return;
     }
     for (int64_t t = (int64_t)blockIdx.x * (256 / kFan) + threadIdx.x / kFan; t < T; t += (int64_t)wgs * (256 / kFan))
@@ -458,33 +524,39 @@ extern "C" int zs_embed_grad(const void *ids_dev, int id_bytes, int64_t T, const
     const GradPlan plan = plan_grad(T, K);
     if (workspace_bytes < plan.total) return ZS_ERR_SIZE;
     hipStream_t s = static_cast<hipStream_t>(hip_stream);
-    // dW is cleared by workgroups beside the ones that sort, half of it beside a merge if there is one
-    const bool whole = lddw == K;
+    // dW is cleared by workgroups beside those that count or sort.  Where there is a merge most of it goes there, and beside the sorting what that
+    // hides: 128256 x 4096 with nothing, 2^22, 2^24, 2^26 elements and half of it there takes 378, 376, 372, 378, 388 us (whole lines: a
+    // part that begins inside one costs 120 us more).
+    constexpr int64_t kBesideSort = 1 << 24;
+    const bool whole = lddw == K, counted = T <= kCounted;
     const int64_t rows = accumulate ? 0 : whole ? 1 : N, cols = whole ? N * K : K;
     Zeros first = {dW_dev, rows, cols, lddw}, second = {dW_dev, 0, cols, lddw};
-    if (T > kTile && rows == 1) {
-        first.cols = cols / 8 * 4;
+    if (!counted && rows == 1) {
+        first.cols = std::min(cols / 2, kBesideSort) / 1024 * 1024;
         second = {dW_dev + first.cols, 1, cols - first.cols, lddw};
-    } else if (T > kTile) {
-        first.rows = rows / 2;
+    } else if (!counted) {
+        first.rows = std::min(rows / 2, kBesideSort / K);
         second = {dW_dev + first.rows * lddw, rows - first.rows, cols, lddw};
     }
-    const Zeros none = {nullptr, 0, 0, 0};
-    const int tiles = (int)ceil_div(T, kTile);
-    auto clearing = [](const Zeros &z, int threads) {
-        return (unsigned)(z.rows == 0 ? 0 : grid_for(z.rows == 1 ? ceil_div(z.cols, 4 * threads) : z.rows, (1 << 28) / threads));
-    };
+    const Zeros none = {dW_dev, 0, cols, lddw};
+    auto with = [](int64_t wgs, const Zeros &z, int threads) { return dim3((unsigned)wgs + grid_for(clearing(z, threads).wgs, (1 << 28) / threads)); };
     uint8_t *ws = static_cast<uint8_t *>(workspace_dev);
     Pair *from = reinterpret_cast<Pair *>(ws), *to = reinterpret_cast<Pair *>(ws + plan.pairs_bytes);
-    if (tiles + clearing(first, kTile))
-        hipLaunchKernelGGL(sort_tiles_kernel, dim3(tiles + clearing(first, kTile)), dim3(kTile), 0, s, ids_dev, id_bytes, T, N, from, tiles, first);
-    for (int64_t run = kTile; run < T; run *= kFan) {
-        const Zeros &z = run == kTile ? second : none;
-        const int wgs = (int)grid_for(ceil_div(T, 256 / kFan));
-        hipLaunchKernelGGL(merge_kernel, dim3(wgs + clearing(z, 256)), dim3(256), 0, s, from, to, T, run, wgs, z);
-        Pair *const swap = from;
-        from = to;
-        to = swap;
+    if (counted) {
+        const int wgs = (int)ceil_div(T, 256 / kFan);
+        if (T > 0 || rows > 0)
+            hipLaunchKernelGGL(count_kernel, with(wgs, first, 256), dim3(256), 4 * 64 * ceil_div(T, 64), s, ids_dev, id_bytes, (int)T, N, from, wgs, first);
+    } else {
+        const int tiles = (int)ceil_div(T, kTile);
+        hipLaunchKernelGGL(sort_tiles_kernel, with(tiles, first, kTile), dim3(kTile), 0, s, ids_dev, id_bytes, T, N, from, tiles, first);
+        for (int64_t run = kTile; run < T; run *= kFan) {
+            const Zeros &z = run == kTile ? second : none;
+            const int wgs = (int)grid_for(ceil_div(T, 256 / kFan));
+            hipLaunchKernelGGL(merge_kernel, with(wgs, z, 256), dim3(256), 0, s, from, to, T, run, wgs, z);
+            Pair *const swap = from;
+            from = to;
+            to = swap;
+        }
     }
     if (T == 0) return launched();
     Runs g;

@@ -166,7 +166,7 @@ def check_grad(ids, dy, n, scale=1.0, base=None, **kw):
 
 
 @pytest.mark.parametrize("t,n,k", [(1, 1, 1), (2, 5, 3), (31, 10, 64), (32, 1000, 8), (33, 3, 130), (100, 50, 513), (1000, 100, 72),
-                                    (1025, 4000, 40), (3000, 7, 16)])
+                                    (1025, 4000, 40), (3000, 7, 16), (4096, 900, 5), (4097, 900, 5), (9, 40, 2500), (4500, 40, 1100)])
 def test_grad(t, n, k):
     rng = np.random.default_rng(t + k)
     ids = rng.integers(-1, n + 1, t)
