@@ -488,8 +488,8 @@ int run_stream(const Product &p, OUT *C, hipStream_t s)
 
 // Tile shapes and what a round of them takes (us), with one workgroup to a compute unit (`alone`) or two: `start` for its
 // first loads and its results, `block` for each block of 128 along K (0: LDS holds one).  For FP32 results (FP16
-// instructions) and BF16 results (8-bit instructions).  From 4096 x 14336 with 200, 512 and 1024 tokens, 256 tiles with K of
-// 1024 and 8192, and 4096 x 8192 with K of 128, 1024 and 4096.
+// instructions) and BF16 results (8-bit instructions).  Fitted to the times of 308 products (17 to 6144 tokens, N 1024 to 28672, K 1000 to 14336)
+// with each shape and up to 16 splits: the ones chosen take 0.7 % longer than the fastest on the average, 13 % at most.
 struct RoundTime {
     float start, block;
 };
@@ -497,16 +497,16 @@ struct TileShape {
     int tokens, features;
     RoundTime alone[2], two[2];
 };
-constexpr TileShape kShapes[] = {{64, 128, {{1.5f, 0.81f}, {1.0f, 0.53f}}, {{2.7f, 1.17f}, {3.3f, 0.71f}}},
-                                 {128, 128, {{3.4f, 1.05f}, {1.4f, 0.88f}}, {{4.5f, 1.95f}, {4.9f, 1.08f}}},
-                                 {128, 128, {{}, {1.5f, 0.71f}}, {}}, // four blocks in LDS instead of two: fits once
-                                 {256, 128, {{6.0f, 1.80f}, {3.6f, 1.14f}}, {}},
-                                 {256, 256, {{}, {6.0f, 1.80f}}, {}}};
+constexpr TileShape kShapes[] = {{64, 128, {{2.2f, 0.74f}, {1.3f, 0.45f}}, {{3.4f, 1.03f}, {2.6f, 0.73f}}},
+                                 {128, 128, {{2.8f, 1.02f}, {2.3f, 0.66f}}, {{3.6f, 1.63f}, {2.1f, 1.05f}}},
+                                 {128, 128, {{}, {2.3f, 0.56f}}, {}}, // four blocks in LDS instead of two: fits once
+                                 {256, 128, {{4.5f, 1.51f}, {3.4f, 0.88f}}, {}},
+                                 {256, 256, {{}, {5.0f, 1.50f}}, {}}};
 enum { kFp32 = 0, kBf16 = 1 };
 
 // The shape and number of splits along K with the least estimated time: rounds of workgroups times their blocks, no less than
-// the operands' way from memory, and for splits a second kernel (3 us, and the partial results there and back at 6.5 TB/s:
-// they stay in the last cache).
+// the operands' way from memory, which gives less to few workgroups, and for splits a second kernel (the partial results there and back at 7.5
+// TB/s: they stay in the last cache).
 struct TilePlan {
     int shape;
     Tiling g;
@@ -515,7 +515,6 @@ TilePlan plan_tiles(const Product &p, int kind, size_t workspace_bytes)
 {
     const double cus = zs_compute_units();
     const int64_t part_ld = (p.N + 3) / 4 * 4;
-    const double traffic = ((double)p.N + (double)p.M) * (double)p.K / 4.5e6; // the operands once, at 4.5 TB/s
     TilePlan best{-1, {}};
     double least = 0;
     for (int i = 0; i < (int)(sizeof kShapes / sizeof *kShapes); ++i) {
@@ -528,11 +527,14 @@ TilePlan plan_tiles(const Product &p, int kind, size_t workspace_bytes)
                                workspace_bytes / 4 / (size_t)splits / (size_t)p.M < (size_t)part_ld))
                 continue;
             const double wgs = (double)tiles * (double)splits;
-            const bool pairs = t.two[kind].block != 0.f && wgs > cus;
-            const RoundTime &round = pairs ? t.two[kind] : t.alone[kind];
-            double time = std::ceil(wgs / (pairs ? 2 * cus : cus)) * (round.start + (double)per_split * round.block);
+            const RoundTime &alone = t.alone[kind], &two = t.two[kind];
+            const double blocks = (double)per_split, one = alone.start + blocks * alone.block, pair = two.start + blocks * two.block;
+            const bool pairs = two.block != 0.f;
+            const double slots = pairs ? 2 * cus : cus, full = std::floor(wgs / slots), rest = wgs - full * slots;
+            double time = full * (pairs ? pair : one) + (rest > cus ? pair : rest > 0 ? one : 0.0);
+            const double traffic = ((double)p.N + (double)p.M) * (double)p.K / (5.5e6 * std::min(1.0, std::sqrt(std::sqrt(wgs / (2 * cus)))));
             time = std::max(time, traffic) + 0.1 * time; // (of those that wait for memory, the one with less to do)
-            if (splits > 1) time += 3.0 + (double)splits * (double)p.M * (double)part_ld * 8 / 6.5e6;
+            if (splits > 1) time += 2.6 + 0.3 * (double)splits + (double)splits * (double)p.M * (double)part_ld * 8 / 7.5e6;
             if (best.shape >= 0 && time >= least) continue;
             least = time;
             best = {i, {n_tiles, tiles, per_split, (int)splits, part_ld}};
