@@ -63,8 +63,8 @@ __device__ __forceinline__ void store4(uint16_t *p, f32x4 v, int64_t left)
 // Each wave requests its blocks of W, of this tile and the next ones, D ahead, straight into operand registers: a lane
 // takes the chunks of 16 bytes `part` and `part` + 4 of its row, so that a load covers 64 contiguous bytes
 // of sixteen rows.  W is the first operand, so a lane holds four features of one token.  Bound by the weights' way from
-// memory: 28672 x 4096 takes 25 us for one token (4.7 TB/s) and 29 us for sixteen, whose codes in LDS save 6 us
-// over fetching them from the L2 for every tile.
+// memory: FP32 results of 28672 x 4096 take 25 us for one token (4.7 TB/s) and 28 us for sixteen, whose codes in LDS save 6 us
+// over fetching them from the L2 for every tile; below 10 MB of weights by latency (4096 x 1024: 4.4 us).
 constexpr size_t kLds = 160 * 1024;
 constexpr size_t stream_sums(int waves) { return (size_t)2 * waves * 1024; }
 constexpr size_t stream_block(int rows) { return (size_t)rows * (kBlock + 4); } // a block's codes and scales
@@ -475,15 +475,16 @@ __global__ __launch_bounds__(256) void join_kernel(const float *parts, int split
     }
 }
 
-// Whether the kernel for few tokens takes a product: its tokens fit, and a workgroup has few enough tiles that their
-// barriers do not matter (57344 x 8192, 14 tiles each: 112 us, against 93 us by tiles through LDS; 28672 x 4096, 7 each: 29 against 29 to 31,
-// one token 27 against 29).  A product whose tokens do not fit is better off with tiles and splits along K (4096 x
-// 14336, sixteen tokens: 18 us, against 20 in two parts).
 constexpr int kStreamWaves = 16;
-bool few_tokens(const Product &p)
+// Dynamic LDS of the kernel for few tokens.
+size_t stream_lds(const Product &p) { return stream_sums(kStreamWaves) + stream_block((int)p.M) * (size_t)p.k_blocks; }
+
+// Its estimated time (us), or more than any if it cannot take the product.
+double stream_time(const Product &p)
 {
-    return p.M <= 16 && stream_sums(kStreamWaves) + stream_block((int)p.M) * (size_t)p.k_blocks <= kLds &&
-           ceil_div(p.N, 16) <= 8 * (int64_t)zs_compute_units();
+    if (p.M > 16 || stream_lds(p) > kLds) return HUGE_VAL;
+    const double tokens = (double)p.M, blocks = (double)ceil_div(ceil_div(p.N, 16), zs_compute_units()) * (double)p.k_blocks; // of a workgroup
+    return 2.8 + 0.06 * tokens + blocks * (0.095 + 0.0012 * tokens);
 }
 
 template <bool W1, typename OUT>
@@ -492,15 +493,14 @@ int run_stream(const Product &p, OUT *C, hipStream_t s)
     const int rc = allow_lds<stream_kernel<kStreamWaves, 2, W1, OUT>>(kLds);
     if (rc != ZS_OK) return rc;
     const dim3 grid((unsigned)std::min(ceil_div(p.N, 16), (int64_t)zs_compute_units()));
-    const size_t lds = stream_sums(kStreamWaves) + stream_block((int)p.M) * (size_t)p.k_blocks;
-    hipLaunchKernelGGL((stream_kernel<kStreamWaves, 2, W1, OUT>), grid, dim3(64 * kStreamWaves), lds, s, p, C);
+    hipLaunchKernelGGL((stream_kernel<kStreamWaves, 2, W1, OUT>), grid, dim3(64 * kStreamWaves), stream_lds(p), s, p, C);
     return launched();
 }
 
 // Tile shapes and what a round of them takes (us), with one workgroup to a compute unit (`alone`) or two: `start` for its
 // first loads and its results, `block` for each block of 128 along K (0: LDS holds one).  For FP32 results (FP16
-// instructions) and BF16 results (8-bit instructions).  Fitted to the times of 308 products (17 to 6144 tokens, N 1024 to 28672, K 1000 to 14336)
-// with each shape and up to 16 splits: the ones chosen take 0.7 % longer than the fastest on the average, 13 % at most.
+// instructions) and BF16 results (8-bit instructions).  Fitted to the times of 382 products (1 to 6144 tokens, N 1024 to 32768, K 1000 to 14336)
+// with each shape and up to 16 splits: the ones chosen take 0.7 % longer than the fastest on the average, 11 % at most.
 struct RoundTime {
     float start, block;
 };
@@ -508,26 +508,26 @@ struct TileShape {
     int tokens, features;
     RoundTime alone[2], two[2];
 };
-constexpr TileShape kShapes[] = {{64, 128, {{2.2f, 0.74f}, {1.3f, 0.45f}}, {{3.4f, 1.03f}, {2.6f, 0.73f}}},
-                                 {128, 128, {{2.8f, 1.02f}, {2.3f, 0.66f}}, {{3.6f, 1.63f}, {2.1f, 1.05f}}},
-                                 {128, 128, {{}, {2.3f, 0.56f}}, {}}, // four blocks in LDS instead of two: fits once
-                                 {256, 128, {{4.5f, 1.51f}, {3.4f, 0.88f}}, {}},
-                                 {256, 256, {{}, {5.0f, 1.50f}}, {}}};
+constexpr TileShape kShapes[] = {{64, 128, {{2.05f, 0.74f}, {1.8f, 0.46f}}, {{3.25f, 1.05f}, {2.8f, 0.72f}}},
+                                 {128, 128, {{2.7f, 1.05f}, {2.25f, 0.69f}}, {{2.85f, 1.70f}, {2.05f, 1.10f}}},
+                                 {128, 128, {{}, {2.4f, 0.56f}}, {}}, // four blocks in LDS instead of two: fits once
+                                 {256, 128, {{4.25f, 1.52f}, {3.25f, 0.96f}}, {}},
+                                 {256, 256, {{}, {4.8f, 1.45f}}, {}}};
 enum { kFp32 = 0, kBf16 = 1 };
 
 // The shape and number of splits along K with the least estimated time: rounds of workgroups times their blocks, no less than
-// the operands' way from memory, which gives less to few workgroups, and for splits a second kernel (the partial results there and back at 7.5
+// the operands' way from memory, which gives less to few workgroups, and for splits a second kernel (the partial results there and back at 7
 // TB/s: they stay in the last cache).
 struct TilePlan {
     int shape;
+    double time;
     Tiling g;
 };
 TilePlan plan_tiles(const Product &p, int kind, size_t workspace_bytes)
 {
     const double cus = zs_compute_units();
     const int64_t part_ld = (p.N + 3) / 4 * 4;
-    TilePlan best{-1, {}};
-    double least = 0;
+    TilePlan best{-1, 0, {}};
     for (int i = 0; i < (int)(sizeof kShapes / sizeof *kShapes); ++i) {
         const TileShape &t = kShapes[i];
         if (t.alone[kind].block == 0.f) continue;
@@ -543,12 +543,10 @@ TilePlan plan_tiles(const Product &p, int kind, size_t workspace_bytes)
             const bool pairs = two.block != 0.f;
             const double slots = pairs ? 2 * cus : cus, full = std::floor(wgs / slots), rest = wgs - full * slots;
             double time = full * (pairs ? pair : one) + (rest > cus ? pair : rest > 0 ? one : 0.0);
-            const double traffic = ((double)p.N + (double)p.M) * (double)p.K / (5.5e6 * std::min(1.0, std::sqrt(std::sqrt(wgs / (2 * cus)))));
+            const double traffic = ((double)p.N + (double)p.M) * (double)p.K / (6.3e6 * std::min(1.0, std::pow(wgs / (2 * cus), 0.08)));
             time = std::max(time, traffic) + 0.1 * time; // (of those that wait for memory, the one with less to do)
-            if (splits > 1) time += 2.6 + 0.3 * (double)splits + (double)splits * (double)p.M * (double)part_ld * 8 / 7.5e6;
-            if (best.shape >= 0 && time >= least) continue;
-            least = time;
-            best = {i, {n_tiles, tiles, per_split, (int)splits, part_ld}};
+            if (splits > 1) time += 2.45 + 0.33 * (double)splits + (double)splits * (double)p.M * (double)part_ld * 8 / 7e6;
+            if (best.shape < 0 || time < best.time) best = {i, time, {n_tiles, tiles, per_split, (int)splits, part_ld}};
         }
     }
     return best;
@@ -570,10 +568,9 @@ int run_tiles(const Product &p, const Tiling &g, OUT *C, void *workspace, hipStr
 }
 
 template <typename OUT>
-int run_tiled(const Product &p, OUT *C, void *workspace, size_t workspace_bytes, hipStream_t s)
+int run_tiled(const Product &p, const TilePlan &plan, OUT *C, void *workspace, hipStream_t s)
 {
     constexpr bool kExact = std::is_same_v<OUT, float>;
-    const TilePlan plan = plan_tiles(p, kExact ? kFp32 : kBf16, workspace_bytes);
     if constexpr (!kExact) {
         if (plan.shape == 2) return run_tiles<2, 4, 4, 2, 4>(p, plan.g, C, workspace, s);
         if (plan.shape == 4) return run_tiles<4, 8, 4, 2, 2>(p, plan.g, C, workspace, s);
@@ -595,9 +592,15 @@ int run(const uint8_t *A, int64_t lda, const float *SA, int64_t ldsa, const uint
     if (lda > kMaxLd || ldw > kMaxLd) return ZS_ERR_SHAPE; // offsets inside a tile are 32 bits wide
     const Product p = {A, W, SA, SW, lda, ldsa, ldw, ldsw, ldc, M, N, K, ceil_div(K, kBlock), w_rows};
     hipStream_t stream = static_cast<hipStream_t>(hip_stream);
-    if (few_tokens(p)) return w_rows == 1 ? run_stream<true>(p, C, stream) : run_stream<false>(p, C, stream);
     if (!workspace) workspace_bytes = 0;
-    return run_tiled(p, C, workspace, workspace_bytes, stream);
+    // The kernel for few tokens, where it is estimated to be faster (tiles take 2 us more than their plan says).  For 60 products of 1 to 16 tokens this
+    // takes 0.5 % longer than the fastest of all on the average, 6 % at most: for BF16 results it is the one for up to 50 MB of weights or so (16 tokens
+    // x 4096 x 4096 7.8 against 10.2 us, 28672 x 4096 28.7 against 23.6), for FP32 results for all that it can take (28.3 against 29.5).
+    const double few = stream_time(p);
+    TilePlan plan{};
+    if (few < 8 || few <= (plan = plan_tiles(p, std::is_same_v<OUT, float> ? kFp32 : kBf16, workspace_bytes)).time + 2)
+        return w_rows == 1 ? run_stream<true>(p, C, stream) : run_stream<false>(p, C, stream);
+    return run_tiled(p, plan, C, workspace, stream);
 }
 
 } // namespace
