@@ -183,8 +183,8 @@ __global__ __launch_bounds__(64 * NW) void stream_kernel(Product p, OUT *C)
 // A workgroup of WM x WN waves computes (16 TM WM) tokens x (16 TN WN) features over the blocks [kb0, kb1) of K.  Each
 // block's codes and scales go from memory straight to LDS; STAGES - 1 blocks are under way while one is
 // multiplied, and there is one barrier a block.  A row's eight chunks of 16 bytes lie in the order chunk ^ (row % 8), so that
-// the sixteen rows of an operand are read without bank conflicts.  4096 tokens, 28672 x 4096, BF16 results: 444 to 475 us (2.0 to 2.2
-// PFLOP/s); FP32 results 6144 x 4096 x 5003: 251 to 265 us (0.95 to 1.0).  Bound by the matrix instructions (200 us of the former) with the
+// the sixteen rows of an operand are read without bank conflicts.  4096 tokens, 28672 x 4096, BF16 results: 434 to 470 us (2.05 to 2.2
+// PFLOP/s); FP32 results 6144 x 4096 x 5003: 256 to 265 us (0.95 to 1.0).  Bound by the matrix instructions (200 us of the former) with the
 // scaling FMAs, which overlap them by a third only (a wave alone: four FMAs to an instruction, 21 ns, two waves 16.6, bare 13.6), the
 // barrier, and the way of 64 KB a block from the L2.
 constexpr int kRowBytes = 128;
@@ -525,28 +525,36 @@ struct TilePlan {
 };
 TilePlan plan_tiles(const Product &p, int kind, size_t workspace_bytes)
 {
-    const double cus = zs_compute_units();
+    constexpr int kN = sizeof kShapes / sizeof *kShapes;
+    const double cus = zs_compute_units(), operands = ((double)p.N + (double)p.M) * (double)p.K / 6.3e6;
     const int64_t part_ld = (p.N + 3) / 4 * 4;
+    const uint32_t k_blocks = (uint32_t)p.k_blocks;
+    int64_t n_tiles[kN], tiles[kN];
+    for (int i = 0; i < kN; ++i) {
+        n_tiles[i] = ceil_div(p.N, kShapes[i].features);
+        tiles[i] = n_tiles[i] * ceil_div(p.M, kShapes[i].tokens);
+    }
     TilePlan best{-1, 0, {}};
-    for (int i = 0; i < (int)(sizeof kShapes / sizeof *kShapes); ++i) {
-        const TileShape &t = kShapes[i];
-        if (t.alone[kind].block == 0.f) continue;
-        const int64_t n_tiles = ceil_div(p.N, t.features), tiles = n_tiles * ceil_div(p.M, t.tokens);
-        for (int64_t splits = 1; splits <= 16; ++splits) {
-            const int64_t per_split = ceil_div(p.k_blocks, splits);
-            if (splits > 1 && (ceil_div(p.k_blocks, per_split) != splits || per_split < 4 ||
-                               workspace_bytes / 4 / (size_t)splits / (size_t)p.M < (size_t)part_ld))
-                continue;
-            const double wgs = (double)tiles * (double)splits;
-            const RoundTime &alone = t.alone[kind], &two = t.two[kind];
-            const double blocks = (double)per_split, one = alone.start + blocks * alone.block, pair = two.start + blocks * two.block;
+    for (uint32_t splits = 1; splits <= 16; ++splits) {
+        const uint32_t per_split = (k_blocks + splits - 1) / splits;
+        double join = 0;
+        if (splits > 1) {
+            if (per_split < 4) break;
+            if ((k_blocks + per_split - 1) / per_split != splits || workspace_bytes / 4 / splits / (size_t)p.M < (size_t)part_ld) continue;
+            join = 2.45 + 0.33 * splits + (double)splits * (double)p.M * (double)part_ld * 8 / 7e6;
+        }
+        for (int i = 0; i < kN; ++i) {
+            const RoundTime &alone = kShapes[i].alone[kind], &two = kShapes[i].two[kind];
+            const double wgs = (double)tiles[i] * splits;
+            if (alone.block == 0.f || (splits > 1 && wgs > 4 * cus)) continue;
+            const double one = alone.start + per_split * alone.block, pair = two.start + per_split * two.block;
             const bool pairs = two.block != 0.f;
             const double slots = pairs ? 2 * cus : cus, full = std::floor(wgs / slots), rest = wgs - full * slots;
             double time = full * (pairs ? pair : one) + (rest > cus ? pair : rest > 0 ? one : 0.0);
-            const double traffic = ((double)p.N + (double)p.M) * (double)p.K / (6.3e6 * std::min(1.0, std::pow(wgs / (2 * cus), 0.08)));
-            time = std::max(time, traffic) + 0.1 * time; // (of those that wait for memory, the one with less to do)
-            if (splits > 1) time += 2.45 + 0.33 * (double)splits + (double)splits * (double)p.M * (double)part_ld * 8 / 7e6;
-            if (best.shape < 0 || time < best.time) best = {i, time, {n_tiles, tiles, per_split, (int)splits, part_ld}};
+            double traffic = operands;
+            if (wgs < 2 * cus) traffic /= std::sqrt(std::sqrt(std::sqrt(std::sqrt(wgs / (2 * cus)))));
+            time = std::max(time, traffic) + 0.1 * time + join; // (of those that wait for memory, the one with less to do)
+            if (best.shape < 0 || time < best.time) best = {i, time, {n_tiles[i], tiles[i], (int64_t)per_split, (int)splits, part_ld}};
         }
     }
     return best;

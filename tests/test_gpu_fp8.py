@@ -154,7 +154,7 @@ def check_gemm(got, a, sa, w, sw, w_rows, out):
 
 SIZES = [(1, 1, 1), (1, 16, 128), (1, 1000, 4096), (2, 130, 129), (5, 64, 1000), (15, 100, 257), (16, 256, 512), (17, 257, 383), (32, 512, 4100),
          (33, 129, 640), (64, 384, 2048), (65, 70, 300), (100, 1024, 1024), (128, 128, 128), (129, 333, 777), (200, 500, 1500), (255, 260, 256),
-         (256, 512, 1024), (257, 300, 2000), (300, 1000, 130), (513, 769, 640), (1000, 64, 4096), (1024, 1024, 512)]
+         (256, 512, 1024), (257, 300, 2000), (300, 1000, 130), (513, 769, 640), (1000, 64, 4096), (1024, 1024, 512), (7, 5003, 8100)]
 
 
 @pytest.mark.parametrize("w_rows", [128, 1])
