@@ -118,22 +118,23 @@ def lib() -> ctypes.CDLL:
     return _lib
 
 
-def _ptr(x) -> ctypes.c_void_p:
-    if x is None:
-        return ctypes.c_void_p(0)
-    if hasattr(x, "data_ptr"):
-        return ctypes.c_void_p(x.data_ptr())
-    if isinstance(x, np.ndarray):
-        return ctypes.c_void_p(x.ctypes.data)
-    return ctypes.c_void_p(int(x))
+def _ptr(x) -> int | None:
+    """Address of a tensor, an array or a number; None is NULL.  (All entry points declare their arguments' types, so an integer is
+    passed whole; a c_void_p for each would cost as much as the call.)"""
+    if x is None or type(x) is int:
+        return x
+    try:
+        return x.data_ptr()
+    except AttributeError:
+        return x.ctypes.data if isinstance(x, np.ndarray) else int(x)
 
 
-def _stream(stream) -> ctypes.c_void_p:
+def _stream(stream) -> int | None:
     if stream is None:
         import torch
         raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)  # (the Stream object costs 2.6 us, a call of ours 4.5)
         stream = raw(torch.cuda.current_device()) if raw else torch.cuda.current_stream()
-    return ctypes.c_void_p(getattr(stream, "cuda_stream", stream))
+    return getattr(stream, "cuda_stream", stream)
 
 
 def _check(fn: str, rc: int) -> None:
