@@ -291,7 +291,7 @@ int zs_variant_decompress(const zs_variant_desc *d, const void *blob_dev, uint16
 /* ---- 8-bit products ----------------------------------------------------------------------
  * A third storage of a weight matrix, beside the compressed blob and plain BF16: OCP E4M3 codes
  * (one byte, largest value 448, NaN but no Inf) with one FP32 scale for each block of 128 along K.
- * Lossy, unlike the blob; half a BF16 matrix's bytes, and multiplied at twice BF16's rate.
+ * Lossy, unlike the blob; half a BF16 matrix's bytes.
  *   codes   [rows, K], one byte each, in rows of ld bytes, ld % 16 == 0, the matrix 16-byte
  *           aligned.  The rows * ld bytes belong to the matrix; what lies behind K in a row has no
  *           effect on a product.
@@ -320,7 +320,7 @@ int zs_fp8_quantize(const void *X_dev, int x_type, int64_t R, int64_t C, int64_t
                     void *hip_stream);
 
 /* C = A * W^T on codes with scales: C[m,n] = sum over blocks b of K of SA[b,m] * SW[b,n / w_rows] *
- * sum over k in b of A[m,k] * W[n,k].  FP32 accumulation on the matrix cores inside a block,
+ * sum over k in b of A[m,k] * W[n,k].  Whole products, FP32 accumulation on the matrix cores inside a block,
  * the product of the two scales and the sum over the blocks in FP32; C is overwritten.
  *   A_dev, SA_dev  [M, K] codes, blocks of 1 x 128, ldsa >= M                       (device, in)
  *   W_dev, SW_dev  [N, K] codes, blocks of w_rows x 128 (w_rows 1 or 128)           (device, in)
@@ -340,11 +340,7 @@ int zs_fp8_gemm(const uint8_t *A_dev, int64_t lda, const float *SA_dev, int64_t 
                 float *C_dev, int64_t ldc, int64_t M, int64_t N, int64_t K, void *workspace_dev,
                 size_t workspace_bytes, void *hip_stream);
 
-/* zs_fp8_gemm with the result rounded once to BF16 (nearest even), as zs_gemm_bf16 does.  All but the smallest
- * products run on the 8-bit matrix instructions: of each group of eight consecutive codes along K they
- * drop what lies below 2^-13 of the group's largest product before the FP32 sum (about 1e-5 of a
- * result's norm, a hundredth of its rounding to BF16).  zs_fp8_gemm drops nothing, and takes up to
- * twice the time where the matrix instructions bound it. */
+/* zs_fp8_gemm with the result rounded once to BF16 (nearest even), as zs_gemm_bf16 does: the same FP32 sums. */
 int zs_fp8_gemm_bf16(const uint8_t *A_dev, int64_t lda, const float *SA_dev, int64_t ldsa,
                      const uint8_t *W_dev, int64_t ldw, const float *SW_dev, int64_t ldsw, int w_rows,
                      uint16_t *C_dev, int64_t ldc, int64_t M, int64_t N, int64_t K, void *workspace_dev,
