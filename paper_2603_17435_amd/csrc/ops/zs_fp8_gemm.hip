@@ -5,6 +5,7 @@
 
 #include <algorithm>
 #include <cmath>
+#include <type_traits>
 
 using namespace zs_ops;
 
@@ -471,8 +472,8 @@ size_t stream_lds(const Product &p) { return stream_sums(kStreamWaves) + stream_
 double stream_time(const Product &p)
 {
     if (p.M > 16 || stream_lds(p) > kLds) return HUGE_VAL;
-    const double tokens = (double)p.M, blocks = (double)ceil_div(ceil_div(p.N, 16), zs_compute_units()) * (double)p.k_blocks; // of a workgroup
-    return 2.8 + 0.06 * tokens + blocks * (0.095 + 0.0012 * tokens);
+    const double tiles = (double)ceil_div(ceil_div(p.N, 16), zs_compute_units()); // of a workgroup
+    return 2.8 + tiles * (0.37 + (double)p.k_blocks * (0.0956 + 0.00125 * (double)p.M));
 }
 
 template <bool W1, typename OUT>
@@ -578,11 +579,13 @@ int run(const uint8_t *A, int64_t lda, const float *SA, int64_t ldsa, const uint
     const Product p = {A, W, SA, SW, lda, ldsa, ldw, ldsw, ldc, M, N, K, ceil_div(K, kBlock), w_rows};
     hipStream_t stream = static_cast<hipStream_t>(hip_stream);
     if (!workspace) workspace_bytes = 0;
-    // The kernel for few tokens, where it is estimated to be faster (tiles take 2 us more than their plan says).  For 930 products of 1 to 16 tokens this
-    // takes 1.8 % longer than the fastest of all on the average, 36 % at most (11 x 32768 x 1024, BF16 results: 13.6 against 10.0 us).
-    const double few = stream_time(p);
+    // The kernel for few tokens, where it is estimated to be faster (for few tokens tiles take a fifth longer than their plan says, a tenth where BF16
+    // results halve what they write).  For 930 products of 1 to 16 tokens (N 1000 to 32768, K 1000 to 14336) this takes 0.5 % longer than the fastest of
+    // all on the average, 14 % at most.  It is the one for rows of more than 1024 codes or so: one token x 28672 x 8192, FP32 results, 44 us against 54 in
+    // tiles, sixteen tokens x 28672 x 4096 28.1 against 30.8, but 1 x 32768 x 1024 13.2 against 10.5, and its ends of a tile tell.
+    const double few = stream_time(p), tiles_take = std::is_same_v<OUT, float> ? 1.2 : 1.1;
     TilePlan plan{};
-    if (few < 8 || few <= (plan = plan_tiles(p, workspace_bytes)).time + 2)
+    if (few < 8 || few <= (plan = plan_tiles(p, workspace_bytes)).time * tiles_take)
         return w_rows == 1 ? run_stream<true>(p, C, stream) : run_stream<false>(p, C, stream);
     return run_tiled(p, plan, C, workspace, stream);
 }
