@@ -1,6 +1,7 @@
 """Which kernels the 8-bit products launch, without a GPU: the host half of zs_fp8_gemm.hip with a stand-in for the HIP
 runtime (launch_record.cpp) that writes the launches down instead."""
 import os
+import random
 import re
 import subprocess
 
@@ -51,3 +52,37 @@ def launches(program, products):
 def test_few_tokens_take_the_kernel_that_measured_faster(program, out, m, n, k, few):
     (first, *_), = launches(program, [(out, m, n, k, 128, WORKSPACE)])
     assert ("stream_kernel" in first[0]) == few, first
+
+
+TILE = re.compile(r"tiles_kernelILi(\d+)ELi(\d+)ELi(\d+)ELi(\d+)E")
+
+
+def tile_of(symbol):
+    tm, tn, wm, wn = map(int, TILE.search(symbol).groups())
+    return 16 * tm * wm, 16 * tn * wn
+
+
+def splits_of(found, m, n):
+    """Into how many parts K is cut."""
+    tokens, features = tile_of(found[0][0])
+    splits, rest = divmod(found[0][1], -(-m // tokens) * -(-n // features))
+    assert rest == 0 and (splits > 1) == (len(found) == 2) and all("join_kernel" in name for name, _ in found[1:])
+    return splits
+
+
+def test_partial_results_fit_the_workspace_and_more_than_128_mb_is_never_used(program):
+    rng = random.Random(5)
+    sizes = [(rng.randrange(17, 3000), rng.randrange(1, 12000), rng.randrange(1, 15000)) for _ in range(600)]
+    rooms = [0, 256, 1 << 20, WORKSPACE, 64 << 20, 128 << 20, 1 << 30]
+    found = {room: launches(program, [("f32", *s, 128, room) for s in sizes]) for room in rooms}
+    for room in rooms:
+        for (m, n, _), f in zip(sizes, found[room]):
+            splits = splits_of(f, m, n)
+            assert splits == 1 or splits * m * (-(-n // 4) * 4) * 4 <= room
+    assert found[128 << 20] == found[1 << 30]
+    assert found[0] != found[WORKSPACE] != found[128 << 20]
+
+
+def test_a_product_that_uses_more_than_the_usual_workspace(program):
+    small, large = (launches(program, [("bf16", 473, 8901, 13272, 128, room)])[0] for room in (WORKSPACE, 128 << 20))
+    assert splits_of(small, 473, 8901) == 1 and splits_of(large, 473, 8901) > 1

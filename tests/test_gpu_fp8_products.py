@@ -4,12 +4,18 @@ import pytest
 
 from fp8_sizes import PRODUCTS
 from oracle import ops
-from test_gpu_fp8 import gpu_gemm, up
+from test_gpu_fp8 import gpu_gemm, operands, up
 
 pytestmark = pytest.mark.gpu
 
 each_kernel = pytest.mark.parametrize("size", [p[0] for p in PRODUCTS], ids=lambda s: "x".join(map(str, s[:3])))
 each_form = pytest.mark.parametrize("out,w_rows", [("f32", 128), ("f32", 1), ("bf16", 128), ("bf16", 1)])
+
+
+def some(n, step, rng):
+    """The first and last rows (or columns), both sides of a tile's borders, and some others."""
+    at = np.concatenate([[0, n - 1, n - 2], np.arange(step, n, step), np.arange(step, n, step) - 1, rng.integers(0, n, 40)])
+    return np.unique(at[(at >= 0) & (at < n)])
 
 
 @each_form
@@ -34,3 +40,26 @@ def test_large_products_that_cancel_leave_the_small_ones(size, out, w_rows):
     got = gpu_gemm(a, sa, w, sw, w_rows, out, workspace=workspace)
     want = (ops.TABLE[a] @ ops.TABLE[w].T) * sa[0][:, None] * sw[0][np.arange(n) // w_rows]
     assert np.array_equal(got, want), f"{(got != want).sum()} of {got.size}, the first at {np.argwhere(got != want)[:4].tolist()}"
+
+
+def check_some(got, a, sa, w, sw, w_rows, out, step=128):
+    """Within FP32's bounds (those of test_gpu_fp8.py, without what 8-bit instructions would lose) on the first and last rows and
+    columns, both sides of the tiles' borders, and some others."""
+    rng = np.random.default_rng(1)
+    rows, cols = some(a.shape[0], 64, rng), some(w.shape[0], step, rng)
+    ref, total = ops.fp8_gemm(a[rows], sa[:, rows], w[cols], sw[:, cols // w_rows], 1)
+    bound = (131 + sa.shape[0]) * 2.0 ** -23 * total
+    if out == "bf16":
+        bound += 2.0 ** -8 * (np.abs(ref) + bound)
+    off = np.abs(got[np.ix_(rows, cols)] - ref)
+    assert (off <= bound).all(), f"{(off > bound).sum()} of {off.size}, worst {np.nanmax(off / np.maximum(bound, 1e-300))} at {np.argwhere(off > bound)[:4].tolist()}"
+
+
+@pytest.mark.parametrize("out", ["f32", "bf16"])
+def test_more_than_the_usual_workspace(out):
+    """A product that splits K with 128 MB and does not with 32: partial results behind the first 32 MB, the same bits again."""
+    args = operands(473, 8901, 13272, 128, 4)
+    got = gpu_gemm(*args, 128, out, workspace=128 << 20)
+    check_some(got, *args, 128, out)
+    assert np.array_equal(got, gpu_gemm(*args, 128, out, workspace=128 << 20))
+    check_some(gpu_gemm(*args, 128, out), *args, 128, out)
