@@ -7,7 +7,7 @@ import subprocess
 
 import pytest
 
-from fp8_sizes import WORKSPACE
+from fp8_sizes import PRODUCTS, WORKSPACE
 from paper_2603_17435_amd import build as zs_build
 
 HERE = os.path.dirname(os.path.abspath(__file__))
@@ -86,3 +86,25 @@ def test_partial_results_fit_the_workspace_and_more_than_128_mb_is_never_used(pr
 def test_a_product_that_uses_more_than_the_usual_workspace(program):
     small, large = (launches(program, [("bf16", 473, 8901, 13272, 128, room)])[0] for room in (WORKSPACE, 128 << 20))
     assert splits_of(small, 473, 8901) == 1 and splits_of(large, 473, 8901) > 1
+
+
+FORMS = [(out, w_rows) for out in ("f32", "bf16") for w_rows in (128, 1)]
+
+
+@pytest.mark.parametrize("size,tile,split", PRODUCTS)
+def test_sizes_of_the_gpu_tests_reach_the_kernels_they_are_meant_for(program, size, tile, split):
+    for found in launches(program, [(out, *size[:3], w_rows, size[3]) for out, w_rows in FORMS]):
+        if tile is None:
+            assert len(found) == 1 and "stream_kernel" in found[0][0]
+        else:
+            assert tile_of(found[0][0]) == tile and (splits_of(found, *size[:2]) > 1) == split
+
+
+def test_sizes_of_the_gpu_tests_reach_every_kernel(program):
+    every = set(subprocess.run([str(program), "kernels"], capture_output=True, text=True, check=True).stdout.split())
+    found = launches(program, [(out, *size[:3], w_rows, size[3]) for size, _, _ in PRODUCTS for out, w_rows in FORMS])
+    assert every == {name for f in found for name, _ in f} and len(every) == 18
+    unsplit = {f[0][0] for f in found if len(f) == 1}
+    split = {f[0][0] for f in found if len(f) == 2}
+    assert unsplit == {name for name in every if "join_kernel" not in name}  # results straight to C ...
+    assert split == {name for name in every if "tiles_kernel" in name}       # ... and by way of the workspace

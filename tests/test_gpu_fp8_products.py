@@ -63,3 +63,40 @@ def test_more_than_the_usual_workspace(out):
     check_some(got, *args, 128, out)
     assert np.array_equal(got, gpu_gemm(*args, 128, out, workspace=128 << 20))
     check_some(gpu_gemm(*args, 128, out), *args, 128, out)
+
+
+@each_form
+@each_kernel
+def test_every_kernel(size, out, w_rows):
+    """Any codes and scales; everything behind K, the last row and the last column is NaN or has to be left alone."""
+    m, n, k, workspace = size
+    args = operands(m, n, k, w_rows, m + k)
+    got = gpu_gemm(*args, w_rows, out, pad=1, workspace=workspace)
+    check_some(got, *args, w_rows, out)
+    assert np.array_equal(got, gpu_gemm(*args, w_rows, out, workspace=workspace))  # other strides, the same bits
+
+
+@each_form
+@each_kernel
+def test_special_values_in_every_kernel(size, out, w_rows):
+    """A NaN code reaches its row or column and nothing else, a zero scale clears its block, an infinite one gives what the
+    definition gives.  (What the infinite scale meets are whole multiples of 2^-9 below 2^13: zero in FP32 where it is zero.)"""
+    m, n, k, workspace = size
+    a, sa, w, sw = operands(m, n, k, w_rows, k)
+    last = sa.shape[0] - 1
+    column = sw.shape[1] // 2
+    cols = np.arange(n)[np.arange(n) // w_rows == column]
+    a[0, k - 1] = 0x7F
+    w[n - 1, 0] = 0xFF
+    w[np.ix_(cols, range(128 * last, k))] = ops.e4m3(np.array([1.0]))[0]
+    sa[0, m - 1] = 0.0
+    sw[last, column] = np.inf
+    got = gpu_gemm(a, sa, w, sw, w_rows, out, workspace=workspace)
+    ref, _ = ops.fp8_gemm(a, sa, w, sw, w_rows)
+    assert np.isnan(ref[0]).all() and np.isnan(ref[:, n - 1]).all() and np.isinf(ref[1:, cols]).any() == (m > 1)
+    assert np.array_equal(np.isnan(got), np.isnan(ref))
+    inf = np.isinf(ref)
+    assert np.array_equal(np.isinf(got), inf) and np.array_equal(got[inf], ref[inf])
+    if m > 1:
+        keep = np.array([j for j in range(n - 1) if j // w_rows != column])
+        check_some(got[1:, keep], a[1:], sa[:, 1:], w[keep], sw[:, keep // w_rows], 1, out)
