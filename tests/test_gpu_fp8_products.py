@@ -4,6 +4,7 @@ import pytest
 
 from fp8_sizes import PRODUCTS
 from oracle import ops
+from paper_2603_17435_amd import binding
 from test_gpu_fp8 import gpu_gemm, operands, up
 
 pytestmark = pytest.mark.gpu
@@ -100,3 +101,46 @@ def test_special_values_in_every_kernel(size, out, w_rows):
     if m > 1:
         keep = np.array([j for j in range(n - 1) if j // w_rows != column])
         check_some(got[1:, keep], a[1:], sa[:, 1:], w[keep], sw[:, keep // w_rows], 1, out)
+
+
+def test_results_behind_2_to_31_elements():
+    """Small whole numbers, so that every sum is exact; operands' rows far apart."""
+    import torch
+    m, n, k, ld = 70000, 33000, 130, 65536
+    if torch.cuda.mem_get_info()[0] < 48 << 30:
+        pytest.skip("needs 48 GB")
+    gen = torch.Generator(device="cuda").manual_seed(m)
+    codes = torch.from_numpy(ops.e4m3(np.arange(-4, 4))).cuda()
+    a, w = (torch.empty(rows, ld, dtype=torch.uint8, device="cuda") for rows in (m, n))
+    for x in (a, w):
+        x[:, :k] = codes[torch.randint(0, 8, (x.shape[0], k), generator=gen, device="cuda")]
+    sa, sw = torch.full((2, m), 0.5, device="cuda"), torch.full((2, up(n, 128) // 128), 2.0, device="cuda")
+    c = torch.empty(m, n, device="cuda")
+    binding.zs_fp8_gemm(a, sa, w, sw, c, m, n, k, lda=ld, ldw=ld)
+    value = torch.float8_e4m3fn
+    wv = w[:, :k].view(value).double()
+    for rows in (slice(0, 200), slice(32700, 32800), slice(65000, 65100), slice(m - 200, m)):
+        assert torch.equal(c[rows].double(), a[rows, :k].view(value).double() @ wv.t())
+
+
+@pytest.mark.parametrize("transpose", [False, True])
+def test_quantize_more_blocks_than_a_launch_has_workgroups(transpose):
+    """2^20 workgroups of sixteen blocks of a row, or of a tile of 128 x 128, are what a launch takes at a time."""
+    import torch
+    r, c = ((1 << 27) + 77, 1) if transpose else ((1 << 24) + 33, 3)
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    x = (torch.randn(r, c, generator=gen, device="cuda") * 3).to(torch.bfloat16)
+    rows, cols = (c, r) if transpose else (r, c)
+    q = torch.full((rows, up(cols, 16)), 0xAA, dtype=torch.uint8, device="cuda")
+    s = torch.full((up(cols, 128) // 128, rows), -7.0, device="cuda")
+    binding.zs_fp8_quantize(x, binding.ZS_TYPE_BF16, r, c, q, s, transpose=transpose)
+    blocks = torch.zeros(rows, up(cols, 128), device="cuda")
+    blocks[:, :cols] = x.t() if transpose else x
+    blocks = blocks.view(rows, -1, 128)
+    peak = blocks.abs().amax(2)
+    mantissa, exponent = torch.frexp(peak)  # 448 = 0.875 2^9
+    e = torch.where(peak == 0, 0, torch.where(mantissa <= 0.875, exponent - 9, exponent - 8).clamp_min(-126))
+    scale = torch.ldexp(torch.ones_like(peak), e)
+    assert torch.equal(s, scale.t())
+    codes = (blocks / scale[:, :, None]).to(torch.float8_e4m3fn).view(torch.uint8).view(rows, -1)
+    assert torch.equal(q, codes[:, :q.shape[1]])
