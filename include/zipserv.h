@@ -321,7 +321,9 @@ int zs_fp8_quantize(const void *X_dev, int x_type, int64_t R, int64_t C, int64_t
 
 /* C = A * W^T on codes with scales: C[m,n] = sum over blocks b of K of SA[b,m] * SW[b,n / w_rows] *
  * sum over k in b of A[m,k] * W[n,k].  Whole products, FP32 accumulation on the matrix cores inside a block,
- * the product of the two scales and the sum over the blocks in FP32; C is overwritten.
+ * the product of the two scales and the sum over the blocks in FP32; C is overwritten.  (The scales are
+ * multiplied first: a product of theirs below 2^-126 has lost bits, one above FP32's range is infinite, whatever
+ * the sum that it meets.)
  *   A_dev, SA_dev  [M, K] codes, blocks of 1 x 128, ldsa >= M                       (device, in)
  *   W_dev, SW_dev  [N, K] codes, blocks of w_rows x 128 (w_rows 1 or 128)           (device, in)
  *   C_dev          [M, N] float, row stride ldc >= N, ldc % 4 == 0, 16-byte aligned (device, out)

@@ -4,7 +4,7 @@ import pytest
 
 from fp8_sizes import PRODUCTS
 from oracle import ops
-from paper_2603_17435_amd import binding
+from paper_2603_17435_amd import binding, inputs
 from test_gpu_fp8 import gpu_gemm, operands, up
 
 pytestmark = pytest.mark.gpu
@@ -101,6 +101,28 @@ def test_special_values_in_every_kernel(size, out, w_rows):
     if m > 1:
         keep = np.array([j for j in range(n - 1) if j // w_rows != column])
         check_some(got[1:, keep], a[1:], sa[:, 1:], w[keep], sw[:, keep // w_rows], 1, out)
+
+
+@each_form
+@pytest.mark.parametrize("m", [5, 70])
+def test_scales_whose_product_leaves_the_normal_range(m, out, w_rows):
+    """The product of two scales is a number in FP32, subnormal or infinite ones too; a sum that is a whole number is multiplied by it
+    and rounded once (and to BF16)."""
+    n, k = 200, 100
+    rng = np.random.default_rng(m)
+    a, w = ops.e4m3(rng.integers(-16, 17, (m, k))), ops.e4m3(rng.integers(-16, 17, (n, k)))
+    a[1] = 0
+    sa = (rng.uniform(1, 2, (1, m)) * 2.0 ** -70).astype(np.float32)
+    sw = (rng.uniform(1, 2, (1, up(n, w_rows) // w_rows)) * 2.0 ** -70).astype(np.float32)
+    sa[0, :3] = 2.0 ** 100, 2.0 ** 100, 1.5
+    sw[0, -1] = 2.0 ** 100
+    with np.errstate(over="ignore", invalid="ignore"):
+        scale = sa[0][:, None] * sw[0][np.arange(n) // w_rows][None, :]
+        want = ((ops.TABLE[a] @ ops.TABLE[w].T) * scale.astype(np.float64)).astype(np.float32)
+    assert (np.abs(scale[3:, 0]) < 2.0 ** -126).all() and np.isinf(scale[0, -1]) and np.isnan(want[1, -1])
+    if out == "bf16":
+        want = inputs.bf16_to_f32(inputs.f32_to_bf16(want))
+    assert np.array_equal(gpu_gemm(a, sa, w, sw, w_rows, out), want, equal_nan=True)
 
 
 def test_results_behind_2_to_31_elements():
