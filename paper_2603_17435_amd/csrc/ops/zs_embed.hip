@@ -20,9 +20,9 @@ __device__ __forceinline__ int64_t id_at(const void *ids, int id_bytes, int64_t 
 // A wave decodes one token's 64 weights of one BlockTile.  Lane f first stands for FragTile f: where the
 // row's bytes of a FragTile start in H is the number of in-window elements before them, which a prefix sum of the popcounts
 // over the lanes gives.  Then lane c stands for the row's column c and fetches the three
-// plane bytes and the start of the FragTile that holds it.  Per BlockTile 40 to 64 FragTiles' planes of 24 bytes and 64 to 128
-// bytes of the row are read: 5000 frequent and rare tokens of 128256 x 4096 take 81 us for 556 MB, of which about half
-// come from the caches.  Few tokens are bound by latency (32: 2.9 us).
+// plane bytes and the start of the FragTile that holds it.  Per BlockTile 39 to 64 FragTiles' planes of 24 bytes and 64 to 128
+// bytes of the row are read: 5000 frequent and rare tokens of 128256 x 4096 take 81 us for 425 MB, of which about a
+// third comes from the caches.  Few tokens are bound by latency (32: 2.9 us).
 struct Blob {
     const uint8_t *bitmaps;
     const u32x2 *offsets;

@@ -65,7 +65,7 @@ __device__ __forceinline__ void store4(uint16_t *p, f32x4 v, int64_t left)
 // takes the chunks of 16 bytes `part` and `part` + 4 of its row, so that a load covers 64 contiguous bytes
 // of sixteen rows.  W is the first operand, so a lane holds four features of one token.  Bound by the weights' way from
 // memory: FP32 results of 28672 x 4096 take 25 us for one token (4.7 TB/s) and 28 us for sixteen, whose codes in LDS save 6 us
-// over fetching them from the L2 for every tile; below 10 MB of weights by latency (4096 x 1024: 4.4 us).
+// over fetching them from the L2 for every tile; below 10 MB of weights by latency (4096 features of 1024 codes: 3.6 to 4.4 us, 1024 of 4096: 5.2 to 5.8).
 constexpr size_t kLds = 160 * 1024;
 constexpr size_t stream_sums(int waves) { return (size_t)2 * waves * 1024; }
 constexpr size_t stream_block(int rows) { return (size_t)rows * (kBlock + 4); } // a block's codes and scales
@@ -184,8 +184,8 @@ __global__ __launch_bounds__(64 * NW) void stream_kernel(Product p, OUT *C)
 // A workgroup of WM x WN waves computes (16 TM WM) tokens x (16 TN WN) features over the blocks [kb0, kb1) of K.  Each
 // block's codes and scales go from memory straight to LDS; STAGES - 1 blocks are under way while one is
 // multiplied, and there is one barrier a block.  A row's eight chunks of 16 bytes lie in the order chunk ^ (row % 8), so that
-// the sixteen rows of an operand are read without bank conflicts.  4096 tokens, 28672 x 4096, BF16 results: 850 to 930 us (1.03 to 1.13
-// PFLOP/s); FP32 results 6144 x 4096 x 5003, w_rows 1: 256 to 269 us (0.94 to 0.98).  Bound by the matrix instructions (the library's BF16 product
+// the sixteen rows of an operand are read without bank conflicts.  4096 tokens, 28672 x 4096, BF16 results: 827 to 930 us (1.03 to 1.16
+// PFLOP/s); FP32 results 6144 x 4096 x 5003, w_rows 1: 249 to 269 us (0.94 to 1.01).  Bound by the matrix instructions (the library's BF16 product
 // takes 645 us of the former) with the conversions to FP16 (two to a matrix instruction in tiles of 256 x 128) and the scaling FMAs beside them.
 constexpr int kRowBytes = 128;
 
