@@ -59,7 +59,7 @@ def fetch_faults(ins, fetches, stages):
     return found
 
 
-def test_checker_sees_planted_faults():
+def test_planted_faults_are_found():
     fetch, wait, reads, barrier = ("global_load_lds_dwordx4 v1, s[4:5]", True), ("s_waitcnt vmcnt(2)", True), ("s_waitcnt lgkmcnt(0)", True), ("s_barrier", True)
     read, label, again, end = ("ds_read_b128 v[4:7], v9", False), (".LBB0_1:", False), ("s_cbranch_scc1 .LBB0_1", False), ("s_endpgm", False)
     everything = ("s_waitcnt vmcnt(0)", True)  # behind the loop
